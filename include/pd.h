@@ -203,6 +203,97 @@ pd_status pd_kv_cache_get(const pd_kv_cache *cache, int32_t slot, int32_t len, v
                           void *stream);
 
 /*
+ * A paged key/value cache: keys and values in pages of page_size positions, all sequences' pages in one pool that the
+ * caller owns and hands out, as a serving program does that fills its memory (the decode batch that meets the TPOT bound is
+ * limited by what fits; slots of max_len positions each waste what their sequences do not reach).  Nothing is kept by the
+ * library: lengths and page numbers are device arrays that a kernel of the caller may advance, so a step captured into a
+ * graph is replayed while the sequences grow, and pages travel between instances by plain copies.
+ *
+ *   k, v          device [n_pages, n_kv_heads, page_size, head_dim], 16-byte aligned, elements of dtype or, with e4m3 set,
+ *                 OCP E4M3 codes
+ *   k_scales, v_scales   device fp32 [n_pages, n_kv_heads], e4m3 only: an element is scale * value(code).  A scale is a
+ *                 power of two between 2^-60 and 2^120, as pd_paged_append makes them
+ *   page_size     16, 32, 64 or 128;  head_dim 64 or 128;  dtype the type of the rows (e4m3: PD_BF16)
+ */
+typedef struct {
+    void *k, *v;
+    float *k_scales, *v_scales;
+    int32_t n_pages, page_size, n_kv_heads, head_dim;
+    int32_t dtype;   /* pd_dtype */
+    int32_t e4m3;    /* 0 or 1 */
+} pd_paged_kv;
+
+/*
+ * The sequences of a call.  Sequence b owns rows row_starts[b] .. row_starts[b + 1] - 1 of the call's tensors (a chunk of its
+ * prompt, drafted tokens, or one new token); they are the newest of the lens[b] positions that it holds with them, so row i of
+ * n is at position lens[b] - n + i.  Position p lies in slot p % page_size of page page_table[b * table_width + p / page_size].
+ * Rows behind row_starts[n_seqs] belong to no sequence and are left alone, and so is a row whose position would be negative
+ * (an empty slot of a fixed-size batch: length 0); attention gives such a row zeros.
+ * The arrays' contents are not checked on the host, and none of them makes a call touch memory outside its tensors: starts
+ * outside 0 .. n_rows and lengths outside 0 .. table_width * page_size count as the nearest bound, a position whose page number
+ * lies outside 0 .. n_pages - 1 is not stored and reads as zeros, and where sequences' rows overlap attention does nothing.
+ * table_width * page_size is at most 2^30.
+ */
+typedef struct {
+    int32_t n_seqs;              /* 0 .. 4096 */
+    int32_t n_rows;              /* rows of the call's tensors, 0 .. 2^24 */
+    const int32_t *row_starts;   /* device [n_seqs + 1], non-decreasing, or NULL: sequence b is row b */
+    const int32_t *lens;         /* device [n_seqs] */
+    const int32_t *page_table;   /* device [n_seqs, table_width] */
+    int32_t table_width;
+} pd_paged_seqs;
+
+/*
+ * The rows of a pd_paged_append call: device tensors in the cache's dtype, the heads of a row next to each other (head_dim
+ * elements each), strides in elements from row to row, so that they can be parts of one projection's rows.  Pointers are
+ * 16-byte aligned and strides multiples of 16 bytes.  q NULL: no queries.  q_out may be q with the same stride; otherwise
+ * inputs and outputs do not overlap.
+ */
+typedef struct {
+    const void *k, *v;           /* [n_rows, n_kv_heads, head_dim] */
+    const void *q;               /* [n_rows, n_q_heads, head_dim] or NULL */
+    void *q_out;                 /* [n_rows, n_q_heads, head_dim], rotated queries */
+    int64_t k_stride, v_stride, q_stride, q_out_stride;
+    int32_t n_q_heads;
+    float rope_base;             /* 0: keys and queries are stored as they are */
+} pd_paged_rows;
+
+/*
+ * Stores the keys and values of the call's rows at their positions, keys rotated on the way (the layer's rotary embedding:
+ * rotate-half pairing, angle = position * rope_base^(-2i/head_dim)), and writes the queries rotated alike to q_out.  Rotation
+ * in fp32, one rounding to what is stored.
+ * E4M3 pages: with A the largest finite magnitude among the rows that the call brings to a page and head, and s(A) the
+ * smallest power of two with A <= 448 s, at least 2^-60, the page's scale becomes s(A) where the call fills the page's
+ * slot 0 and max(old scale, s(A)) otherwise; codes of the page's earlier positions are then rounded again to the larger
+ * scale (exact except for what becomes subnormal).  New elements are coded as by pd_quantize_rows_e4m3: nearest, ties to
+ * even, saturating at +-448; NaN stays NaN.  Slots behind the sequence's last position are left as they were.
+ * A page that receives rows belongs to one sequence of the call: two sequences may share pages that they only read.
+ * Asynchronous on stream.  Errors: PD_ERR_INVALID_ARG (NULL, misaligned pointers, counts or rope_base out of range),
+ * PD_ERR_SHAPE (sizes, strides), PD_ERR_DTYPE, PD_ERR_DEVICE.
+ */
+pd_status pd_paged_append(const pd_paged_kv *kv, const pd_paged_seqs *seqs, const pd_paged_rows *rows, void *stream);
+
+/*
+ * Causal grouped-query attention of the call's rows over their sequences' positions: out[r, h] = softmax over the positions
+ * 0 .. p of row r of (scale * q[r, h] . k) times v, query head h reading kv head h / (n_q_heads / n_kv_heads).  The rows'
+ * own keys and values are read from the cache like all others (pd_paged_append first).  One row per sequence is a decode
+ * step, several are drafted tokens or a chunk, lens equal to the rows a whole prompt, in any mixture.
+ * q [n_rows, n_q_heads, head_dim] with a row stride in elements as above; out [n_rows, n_q_heads, head_dim] contiguous, 16-byte
+ * aligned.  Scores, softmax and sums in fp32; in bf16 the exponentials are rounded to bf16 before they weigh the values.
+ * Results do not depend on what else is in a page: unused slots, later positions and infinities or NaN in them.
+ * A row without a visible position gets zeros.
+ * workspace: device memory, 16-byte aligned, of at least pd_paged_attention_workspace bytes for the same host-side sizes
+ * (n_rows, n_seqs, table_width, whether row_starts is NULL); it needs no initial value, holds nothing between calls, and is not
+ * used by two calls at once.  The same call gives the same bits every time.  Asynchronous on stream; no allocation.
+ * Errors: as pd_paged_append; PD_ERR_INVALID_ARG also for a workspace that is too small or a scale that is not positive and finite.
+ */
+pd_status pd_paged_attention(const pd_paged_kv *kv, const pd_paged_seqs *seqs, const void *q, int64_t q_stride,
+                             int32_t n_q_heads, float scale, void *out, void *workspace, int64_t workspace_bytes,
+                             void *stream);
+/* Bytes (0 .. some 100 MiB) that the call above needs; host only.  Errors as above; *bytes untouched on error. */
+pd_status pd_paged_attention_workspace(const pd_paged_kv *kv, const pd_paged_seqs *seqs, int32_t n_q_heads, int64_t *bytes);
+
+/*
  * Prefill: the layer forward over a packed batch of n_seqs sequences (T = cu_seqlens[n_seqs]
  * rows; sequence s owns rows cu_seqlens[s] .. cu_seqlens[s+1]-1 and its positions start at 0).
  * This is the operation whose saturated throughput is the paper's maximum prefill throughput

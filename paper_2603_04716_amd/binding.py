@@ -23,7 +23,7 @@ PD_F32, PD_BF16 = 0, 1
 EXPORTS = [
     "pd_layer_create", "pd_layer_create_w8", "pd_layer_create_w8a8", "pd_quantize_rows_e4m3", "pd_gemm_e4m3", "pd_layer_destroy", "pd_layer_reserve", "pd_kv_cache_create", "pd_kv_cache_create_fp8",
     "pd_kv_cache_destroy", "pd_kv_cache_set", "pd_kv_cache_set_len", "pd_kv_cache_len",
-    "pd_kv_cache_set_lens", "pd_kv_cache_get", "pd_profile_enable", "pd_profile_read", "pd_stream_copy", "pd_mfma_probe", "pd_head_create", "pd_head_create_w8", "pd_head_destroy", "pd_embed", "pd_lm_head", "pd_prefill", "pd_prefill_chunk", "pd_decode_step", "pd_decode_step_noalloc", "pd_last_expert_choice", "pd_allocate",
+    "pd_kv_cache_set_lens", "pd_kv_cache_get", "pd_profile_enable", "pd_profile_read", "pd_stream_copy", "pd_mfma_probe", "pd_head_create", "pd_head_create_w8", "pd_head_destroy", "pd_embed", "pd_lm_head", "pd_paged_append", "pd_paged_attention", "pd_paged_attention_workspace", "pd_prefill", "pd_prefill_chunk", "pd_decode_step", "pd_decode_step_noalloc", "pd_last_expert_choice", "pd_allocate",
     "pd_fifo_replay", "pd_mm1_sojourn", "pd_fifo_replay_batched", "pd_prefill_throughput_dp", "pd_mg1_sojourn", "pd_kv_transfer_overhead", "pd_allocate_stages", "pd_status_string", "pd_last_error",
 ]
 
@@ -72,6 +72,23 @@ class pd_allocation(C.Structure):
                 ("curve_non_monotone", C.c_int32)]
 
 
+class pd_paged_kv(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("e4m3", C.c_int32)]
+
+
+class pd_paged_seqs(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("row_starts", C.c_void_p), ("lens", C.c_void_p),
+                ("page_table", C.c_void_p), ("table_width", C.c_int32)]
+
+
+class pd_paged_rows(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("q", C.c_void_p), ("q_out", C.c_void_p),
+                ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("q_stride", C.c_int64), ("q_out_stride", C.c_int64),
+                ("n_q_heads", C.c_int32), ("rope_base", C.c_float)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it with `python paper_2603_04716_amd/build.py` "
                       "(there is no fallback path)")
@@ -90,6 +107,9 @@ lib.pd_allocate.argtypes = [C.c_double] * 5 + [C.POINTER(pd_measured_curves), C.
 lib.pd_mm1_sojourn.argtypes = [C.c_double] * 3 + [C.POINTER(C.c_double)]
 lib.pd_mg1_sojourn.argtypes = [C.c_double] * 3 + [C.POINTER(C.c_double)]
 lib.pd_kv_transfer_overhead.argtypes = ([C.c_double] + [C.c_int32] * 3 + [C.c_double] * 3 + [C.POINTER(C.c_double)])
+lib.pd_paged_append.argtypes = [C.c_void_p] * 4
+lib.pd_paged_attention.argtypes = ([C.c_void_p] * 3 + [C.c_int64, C.c_int32, C.c_float] + [C.c_void_p] * 2 + [C.c_int64, C.c_void_p])
+lib.pd_paged_attention_workspace.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.POINTER(C.c_int64)]
 lib.pd_prefill_throughput_dp.argtypes = [C.c_double] * 4 + [C.c_int32, C.POINTER(C.c_double)]
 
 
@@ -288,6 +308,80 @@ def pd_decode_step_noalloc(layer, hidden, slots, cache, out, router_logits=None)
 def pd_last_expert_choice(layer, rows, expert_idx):
     _check(lib.pd_last_expert_choice(layer, C.c_int32(rows), _ptr(expert_idx), _stream()))
     return expert_idx
+
+
+# ---- paged key/value cache -------------------------------------------------------------------------
+
+def make_paged_kv(k_pages, v_pages, k_scales=None, v_scales=None):
+    """Descriptor of a pool: k_pages, v_pages [n_pages, n_kv_heads, page_size, head_dim] float32 or bfloat16, or (with
+    k_scales, v_scales [n_pages, n_kv_heads] float32) float8_e4m3fn or uint8 codes.  It keeps the tensors alive."""
+    codes = k_pages.dtype in (torch.float8_e4m3fn, torch.uint8)
+    if k_pages.dtype not in (torch.float32, torch.bfloat16) and not codes:
+        raise ValueError("make_paged_kv: pages are float32, bfloat16, or float8_e4m3fn / uint8 codes")
+    if (v_pages.dtype != k_pages.dtype or k_pages.dim() != 4 or v_pages.shape != k_pages.shape or not k_pages.is_contiguous()
+            or not v_pages.is_contiguous()):
+        raise ValueError("make_paged_kv: k_pages and v_pages are contiguous [n_pages, n_kv_heads, page_size, head_dim] tensors of one type")
+    for t in (k_scales, v_scales):
+        if (t is not None) != codes or (codes and (t.dtype != torch.float32 or t.shape != k_pages.shape[:2] or not t.is_contiguous())):
+            raise ValueError("make_paged_kv: codes, and only they, have scales: contiguous float32 [n_pages, n_kv_heads]")
+    n, h, ps, hd = k_pages.shape
+    kv = pd_paged_kv(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr() if codes else None, v_scales.data_ptr() if codes else None,
+                     n, ps, h, hd, PD_F32 if k_pages.dtype == torch.float32 else PD_BF16, int(codes))
+    kv.tensors = (k_pages, v_pages, k_scales, v_scales)
+    return kv
+
+
+def make_paged_seqs(lens, page_table, row_starts=None, n_rows=None):
+    """Descriptor of a call's sequences: device int32 tensors lens [n_seqs], page_table [n_seqs, table_width] and row_starts
+    [n_seqs + 1] (None: one row each); n_rows: rows of the call's tensors (default: n_seqs, needed with row_starts)."""
+    for t in (lens, page_table, row_starts):
+        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
+            raise ValueError("make_paged_seqs: contiguous int32 tensors")
+    n = lens.shape[0]
+    if page_table.dim() != 2 or page_table.shape[0] != n or (row_starts is not None and (row_starts.shape != (n + 1,) or n_rows is None)):
+        raise ValueError("make_paged_seqs: page_table [n_seqs, table_width], row_starts [n_seqs + 1] together with n_rows")
+    seqs = pd_paged_seqs(n, n if n_rows is None else int(n_rows), None if row_starts is None else row_starts.data_ptr(), lens.data_ptr(),
+                         page_table.data_ptr(), page_table.shape[1])
+    seqs.tensors = (lens, page_table, row_starts)
+    return seqs
+
+
+def _paged_stride(who, t, kv, seqs, heads):
+    """Row stride of t [n_rows, heads, head_dim] whose rows hold their heads next to each other."""
+    hd = kv.head_dim
+    if (t.dtype != (torch.float32 if kv.dtype == PD_F32 else torch.bfloat16) or t.dim() != 3 or t.shape != (seqs.n_rows, heads, hd)
+            or (t.stride(2) != 1 or (heads > 1 and t.stride(1) != hd)) and t.numel() > 0):
+        raise ValueError(f"{who}: tensors are [n_rows, heads, head_dim] in the cache's row type, the heads of a row next to each other")
+    return t.stride(0) if seqs.n_rows > 1 else heads * hd
+
+
+def pd_paged_append(kv, seqs, k, v, rope_base=0.0, q=None, q_out=None):
+    """k, v [n_rows, n_kv_heads, head_dim] into the pages of kv; q [n_rows, n_q_heads, head_dim] rotated into q_out."""
+    who, h = "pd_paged_append", kv.n_kv_heads
+    rows = pd_paged_rows(k.data_ptr(), v.data_ptr(), None, None, _paged_stride(who, k, kv, seqs, h), _paged_stride(who, v, kv, seqs, h), 0, 0,
+                         0, rope_base)
+    if q is not None:
+        rows.q, rows.q_out, rows.n_q_heads = q.data_ptr(), q_out.data_ptr(), q.shape[1]
+        rows.q_stride, rows.q_out_stride = _paged_stride(who, q, kv, seqs, q.shape[1]), _paged_stride(who, q_out, kv, seqs, q.shape[1])
+    _check(lib.pd_paged_append(C.byref(kv), C.byref(seqs), C.byref(rows), _stream()))
+
+
+def pd_paged_attention_workspace(kv, seqs, n_q_heads):
+    """Bytes of workspace that pd_paged_attention needs for calls of these sizes."""
+    n = C.c_int64()
+    _check(lib.pd_paged_attention_workspace(C.byref(kv), C.byref(seqs), n_q_heads, C.byref(n)))
+    return n.value
+
+
+def pd_paged_attention(kv, seqs, q, out, workspace, scale=None):
+    """out [n_rows, n_q_heads, head_dim] (contiguous) = attention of q over the pages; scale: 1 / sqrt(head_dim) by default."""
+    stride = _paged_stride("pd_paged_attention", q, kv, seqs, q.shape[1])
+    if out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+        raise ValueError("pd_paged_attention: out is a contiguous tensor like q")
+    _check(lib.pd_paged_attention(C.byref(kv), C.byref(seqs), q.data_ptr(), stride, q.shape[1],
+                                  kv.head_dim ** -0.5 if scale is None else scale, out.data_ptr(),
+                                  workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
+    return out
 
 
 # ---- host entry points -----------------------------------------------------------------------------

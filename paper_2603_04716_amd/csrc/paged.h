@@ -1,0 +1,78 @@
+// Paged key/value cache: what its kernels share (internal, not part of the C ABI).
+#pragma once
+#include "pd_internal.h"
+
+namespace pd {
+
+enum PagedKind { PAGED_BF16 = 0, PAGED_E4M3 = 1, PAGED_F32 = 2 };
+constexpr int kPagedMaxSeqs = 4096;
+constexpr float kPagedMinScale = 0x1p-60f;      // smallest scale of an E4M3 page: its inverse is an ordinary fp32 number
+
+// The pages and the sequences of a call.  starts, lens and the table come from device memory and are not known on the
+// host, so every value read from them is brought into its range before it is used: no content of theirs makes a kernel
+// leave the tensors.
+struct PagedView {
+    void *k, *v;                     // [n_pages][Hkv][1 << ps_log][hd]
+    float *k_scales, *v_scales;      // [n_pages][Hkv] (E4M3)
+    const int32_t *starts;           // [n_seqs + 1], or null: sequence b is row b
+    const int32_t *lens;             // [n_seqs]
+    const int32_t *table;            // [n_seqs][width]
+    int32_t n_seqs, n_rows, width, ps_log, n_pages, Hkv;
+};
+
+__device__ __forceinline__ int paged_start(const PagedView &p, int b)
+{
+    return p.starts ? min(max(p.starts[b], 0), p.n_rows) : b;
+}
+// rows of sequence b (a host check keeps n_rows >= n_seqs where starts is null)
+__device__ __forceinline__ int paged_rows(const PagedView &p, int b, int start)
+{
+    return p.starts ? max(paged_start(p, b + 1) - start, 0) : 1;
+}
+__device__ __forceinline__ int paged_len(const PagedView &p, int b)
+{
+    return min(max(p.lens[b], 0), p.width << p.ps_log);
+}
+
+struct PagedAppendArgs {
+    PagedView p;
+    const void *q, *k, *v;                           // rows; q null: keys and values only
+    void *q_out;
+    int64_t q_stride, k_stride, v_stride, q_out_stride;   // elements from row to row
+    int32_t Hq, rope;                                // rope 0: keys and queries are stored as they are
+    double turns[64];                                // base^(-2c / hd) / (2 pi): turns per position of channel pair c
+};
+hipError_t launch_paged_append(int kind, int hd, const PagedAppendArgs &a, hipStream_t s);
+
+// Partial results of sequences whose keys are divided over several workgroups, for one attention kernel.  A unit is a
+// tile of query rows of one sequence and kv head.
+struct PagedParts {
+    int32_t *head;      // [0]: units that were split in this call
+    int32_t *desc;      // [cap_units][8]: first partial, partials, stride, first row of the sequence, first (token, head) row of
+                        // the unit, (token, head) rows of the sequence, kv head
+    float *ml;          // [cap_items][rows][2] running maximum (log2 domain) and sum
+    float *o;           // [cap_items][rows][hd] unnormalised
+    int32_t cap_units, rows;
+};
+struct PagedAttnArgs {
+    PagedView p;
+    const void *q;
+    int64_t q_stride;
+    void *out;                       // [n_rows][Hq][hd]
+    int32_t Hq, G;                   // G = Hq / Hkv
+    float scale;
+    int32_t chunk_min, target;       // fewest keys of a chunk; (unit, chunk) items to aim for
+    PagedParts parts;
+};
+// What a call needs of its workspace, and where it lies: host fields of the call only.
+struct PagedAttnPlan {
+    int rows;                        // query rows of a unit
+    int chunk_min, target;
+    int cap_units, cap_items;        // split units and their partials: bounds
+    size_t off_desc, off_ml, off_o, bytes;
+    bool merge;                      // some sequence may be split
+};
+PagedAttnPlan paged_attn_plan(int kind, int hd, const PagedView &p, int Hq);
+hipError_t launch_paged_attention(int kind, int hd, PagedAttnArgs a, const PagedAttnPlan &plan, char *ws, hipStream_t s);
+
+}  // namespace pd
