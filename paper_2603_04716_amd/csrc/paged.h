@@ -48,11 +48,11 @@ hipError_t launch_paged_append(int kind, int hd, const PagedAppendArgs &a, hipSt
 // tile of query rows of one sequence and kv head.
 struct PagedParts {
     int32_t *head;      // [0]: units that were split in this call
-    int32_t *desc;      // [cap_units][8]: first partial, partials, stride, first row of the sequence, first (token, head) row of
-                        // the unit, (token, head) rows of the sequence, kv head
+    int32_t *desc;      // [cap_units][8]: first partial, partials, first row of the sequence, first (token, head) row of the
+                        // unit, (token, head) rows of the sequence, kv head, position of the sequence's first row
     float *ml;          // [cap_items][rows][2] running maximum (log2 domain) and sum
     float *o;           // [cap_items][rows][hd] unnormalised
-    int32_t cap_units, rows;
+    int32_t rows;       // query rows of a unit
 };
 struct PagedAttnArgs {
     PagedView p;
@@ -61,18 +61,25 @@ struct PagedAttnArgs {
     void *out;                       // [n_rows][Hq][hd]
     int32_t Hq, G;                   // G = Hq / Hkv
     float scale;
+    int32_t rows_above, rows_most;   // this kernel's sequences: more (token, head) rows than the one, at most the other
     int32_t chunk_min, target;       // fewest keys of a chunk; (unit, chunk) items to aim for
     PagedParts parts;
 };
-// What a call needs of its workspace, and where it lies: host fields of the call only.
-struct PagedAttnPlan {
+// How one of the two kernels is launched, and its part of the workspace: from the host's fields of the call alone.
+struct PagedAttnPart {
+    bool used, merge;                // launched at all; some of its sequences may be split
     int rows;                        // query rows of a unit
-    int chunk_min, target;
-    int cap_units, cap_items;        // split units and their partials: bounds
-    size_t off_desc, off_ml, off_o, bytes;
-    bool merge;                      // some sequence may be split
+    int rows_above, rows_most, chunk_min, target;
+    int64_t units;                   // at most
+    int cap_units, cap_items;        // split units and their partials: at most
+    size_t off_head, off_desc, off_ml, off_o;
+};
+struct PagedAttnPlan {
+    PagedAttnPart few, many;
+    size_t bytes;
 };
 PagedAttnPlan paged_attn_plan(int kind, int hd, const PagedView &p, int Hq);
-hipError_t launch_paged_attention(int kind, int hd, PagedAttnArgs a, const PagedAttnPlan &plan, char *ws, hipStream_t s);
+hipError_t launch_paged_attention(int kind, int hd, const PagedAttnArgs &a, const PagedAttnPlan &plan, char *ws, hipStream_t s);
+hipError_t launch_paged_tiles(int kind, int hd, const PagedAttnArgs &a, unsigned grid, hipStream_t s);
 
 }  // namespace pd

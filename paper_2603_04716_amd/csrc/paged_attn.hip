@@ -18,7 +18,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "paged.h"
+#include "paged_items.h"
 
 namespace pd {
 
@@ -27,95 +27,6 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-
-__device__ __forceinline__ float pexp2(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// ---- the division of the call's keys into items ------------------------------------------------------------------------
-//
-// Lengths are known on the device alone, so every workgroup works the division out for itself: the keys that all units
-// have to read, divided by the items aimed for, is the chunk; a sequence of len keys and U units makes U ceil(len / chunk)
-// items, and since U (len / chunk + 1) <= 2 U len / chunk where there is more than one chunk, the split ones are at most
-// twice the items aimed for.  pre[0 .. 2][b]: items, split items and split units (per kv head) ahead of sequence b.
-struct PagedItems {
-    int chunk, total, split_items, split_units;
-};
-template <int NT>
-__device__ __forceinline__ long block_sum(long v, long *red)
-{
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    long s = 0;
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) s += red[w];
-    return s;
-}
-// sum over the threads below this one
-template <int NT>
-__device__ __forceinline__ int block_scan(int v, int *red)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int inc = v;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int u = __shfl_up(inc, off, 64);
-        if (lane >= off) inc += u;
-    }
-    __syncthreads();
-    if (lane == 63) red[wave] = inc;
-    __syncthreads();
-    int base = 0;
-    for (int w = 0; w < wave; ++w) base += red[w];
-    return base + inc - v;
-}
-// units of sequence b
-template <int R>
-__device__ __forceinline__ int paged_units(const PagedAttnArgs &a, int b)
-{
-    return (paged_rows(a.p, b, paged_start(a.p, b)) * a.G + R - 1) / R;
-}
-template <int R, int NT>
-__device__ __forceinline__ PagedItems paged_divide(const PagedAttnArgs &a, int *pre, void *red)
-{
-    const int n = a.p.n_seqs, per = (n + NT - 1) / NT, b0 = min((int)threadIdx.x * per, n), b1 = min(b0 + per, n);
-    long keys = 0, rows = 0;
-    for (int b = b0; b < b1; ++b) {
-        keys += (long)paged_units<R>(a, b) * paged_len(a.p, b);
-        rows += paged_rows(a.p, b, paged_start(a.p, b));
-    }
-    keys = block_sum<NT>(keys, (long *)red) * a.p.Hkv;
-    rows = block_sum<NT>(rows, (long *)red);
-    PagedItems r = {64, 0, 0, 0};
-    if (rows > a.p.n_rows) return r;                 // the sequences' rows overlap: no such call, and nothing is done
-    r.chunk = (int)min((max((keys + a.target - 1) / a.target, (long)a.chunk_min) + 63) & ~63l, 1l << 30);
-    int c[3] = {0, 0, 0};
-    for (int b = b0; b < b1; ++b) {
-        const int u = paged_units<R>(a, b), nc = max((paged_len(a.p, b) + r.chunk - 1) / r.chunk, 1);
-        c[0] += u * nc;
-        if (nc > 1) {
-            c[1] += u * nc;
-            c[2] += u;
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-        int run = block_scan<NT>(c[k], (int *)red);
-        int *q = pre + k * (n + 1);
-        for (int b = b0; b < b1; ++b) {
-            q[b] = run;
-            const int u = paged_units<R>(a, b), nc = max((paged_len(a.p, b) + r.chunk - 1) / r.chunk, 1);
-            run += k == 0 ? u * nc : nc == 1 ? 0 : k == 1 ? u * nc : u;
-        }
-        if (b1 == n && b0 < n) q[n] = run;
-    }
-    __syncthreads();
-    r.total = pre[n];
-    r.split_items = pre[2 * n + 1];
-    r.split_units = pre[3 * n + 2];
-    return r;
-}
 
 // ---- one step of NKB * 16 keys in registers -------------------------------------------------------------------------------
 //
@@ -400,221 +311,211 @@ __global__ __launch_bounds__(256, KIND == PAGED_F32 ? 1 : 2) void paged_rows_ker
     constexpr int R = 16 * NR, NKB = S::NKB, KS = 16 * NKB, CPL = S::CPL, NQ = S::NQ, LD = HD + 4;
     extern __shared__ __attribute__((aligned(16))) float sm[];
     float *os = sm, *ml = sm + kWaves * R * LD;      // per wave: O [R][LD]; (maximum, sum) [R]
-    int *pre = (int *)(ml + kWaves * R * 2);         // [3][n_seqs + 1]
     __shared__ long red[kWaves];
+    __shared__ PagedFound found;
     const PagedView &p = a.p;
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, kg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const PagedItems it = paged_divide<R, 256>(a, pre, red);
-    const int *pre_split = pre + p.n_seqs + 1, *pre_unit = pre_split + p.n_seqs + 1;
+    const PagedItems it = paged_divide<R, 256>(a, red);
     if (blockIdx.x == 0 && tid == 0 && a.parts.head) a.parts.head[0] = it.split_units * p.Hkv;
     const float sl2e = a.scale * 1.4426950408889634f;
 
-    for (int item = blockIdx.x; item < it.total * p.Hkv; item += gridDim.x) {
-        const int t = item / p.Hkv, g = item - t * p.Hkv;
-        int b = 0;
-        for (int hi = p.n_seqs; hi - b > 1;) {       // last sequence whose items start at or before t
-            const int mid = (b + hi) >> 1;
-            if (pre[mid] <= t) b = mid; else hi = mid;
-        }
-        b = __builtin_amdgcn_readfirstlane(b);
-        const int start = paged_start(p, b), rows = paged_rows(p, b, start), len = paged_len(p, b);
-        const int units = (rows * a.G + R - 1) / R, nc = max((len + it.chunk - 1) / it.chunk, 1);
-        // row tiles that read the same keys are neighbours, the one that sees most first
-        const int c = (t - pre[b]) / units, u = units - 1 - (t - pre[b] - c * units);
-        const int r0 = u * R, nrows = min(R, rows * a.G - r0);
-        const int before = len - rows;               // position of the sequence's first row (negative: it is not held)
-        const int vis_min = before + r0 / a.G + 1, vis_max = max(before + (r0 + nrows - 1) / a.G + 1, 0);
-        const int nc_u = max((vis_max + it.chunk - 1) / it.chunk, 1);
-        if (c >= nc_u) continue;
-        const int c0 = c * it.chunk, c1 = min(vis_max, c0 + it.chunk);
+    const int t = blockIdx.x / p.Hkv, g = blockIdx.x - t * p.Hkv;
+    if (t >= it.total) return;
+    paged_find<R>(a, it, t, &found);
+    const int b = __builtin_amdgcn_readfirstlane(found.seq), units = __builtin_amdgcn_readfirstlane(found.units);
+    const int nc = __builtin_amdgcn_readfirstlane(found.chunks), at = __builtin_amdgcn_readfirstlane(found.at);
+    const int start = paged_start(p, b), rows = paged_rows(p, b, start), len = paged_len(p, b);
+    // row tiles that read the same keys are neighbours, the one that sees most first
+    const int c = at / units, u = units - 1 - (at - c * units);
+    const int r0 = u * R, nrows = min(R, rows * a.G - r0);
+    const int before = len - rows;               // position of the sequence's first row (negative: it is not held)
+    const int vis_min = before + r0 / a.G + 1, vis_max = max(before + (r0 + nrows - 1) / a.G + 1, 0);
+    const int nc_u = max((vis_max + it.chunk - 1) / it.chunk, 1);
+    if (c >= nc_u) return;
+    const int c0 = c * it.chunk, c1 = min(vis_max, c0 + it.chunk);
 
-        typename S::qfrag q[NR][NQ];
-        int limit[NR];                               // the row sees keys 0 .. limit - 1
+    typename S::qfrag q[NR][NQ];
+    int limit[NR];                               // the row sees keys 0 .. limit - 1
 #pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            const int row = r0 + 16 * r + n, tok = row / a.G;
-            const bool ok = row < r0 + nrows;
-            limit[r] = ok ? before + tok + 1 : 0;
-            S::no_q(q[r]);
-            if (ok) S::load_q((const T *)a.q + (start + tok) * a.q_stride + (g * a.G + row - tok * a.G) * HD, kg, q[r]);
+    for (int r = 0; r < NR; ++r) {
+        const int row = r0 + 16 * r + n, tok = row / a.G;
+        const bool ok = row < r0 + nrows;
+        limit[r] = ok ? before + tok + 1 : 0;
+        S::no_q(q[r]);
+        if (ok) S::load_q((const T *)a.q + (start + tok) * a.q_stride + (g * a.G + row - tok * a.G) * HD, kg, q[r]);
+    }
+    f32x4 o[NR][CPL];
+    float m_run[NR], l_run[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        m_run[r] = -INFINITY;
+        l_run[r] = 0.f;
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) o[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int32_t *pages = p.table + (size_t)b * p.width;
+    for (int k0 = c0 + wave * KS; k0 < c1; k0 += kWaves * KS) {
+        S st;
+        bool gone[NKB];
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb) {
+            const int key = k0 + 16 * kb, at = min(key, len - 1);
+            const int id = pages[at >> p.ps_log];
+            gone[kb] = id < 0 || id >= p.n_pages;
+            const size_t unit = (size_t)(gone[kb] ? 0 : id) * p.Hkv + g;
+            const size_t off = ((unit << p.ps_log) + (key & ((1 << p.ps_log) - 1))) * HD;
+            st.load(kb, (const typename S::elem *)p.k + off, (const typename S::elem *)p.v + off,
+                    KIND == PAGED_E4M3 ? p.k_scales[unit] : 1.f, KIND == PAGED_E4M3 ? p.v_scales[unit] : 1.f, n, kg);
         }
-        f32x4 o[NR][CPL];
-        float m_run[NR], l_run[NR];
 #pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            m_run[r] = -INFINITY;
-            l_run[r] = 0.f;
+        for (int kb = 0; kb < NKB; ++kb) {
+            if (gone[kb]) {                      // a page that is not there reads as zeros
+                st.clear_keys(kb);
 #pragma unroll
-            for (int i = 0; i < CPL; ++i) o[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-        const int32_t *pages = p.table + (size_t)b * p.width;
-        for (int k0 = c0 + wave * KS; k0 < c1; k0 += kWaves * KS) {
-            S st;
-            bool gone[NKB];
-#pragma unroll
-            for (int kb = 0; kb < NKB; ++kb) {
-                const int key = k0 + 16 * kb, at = min(key, len - 1);
-                const int id = pages[at >> p.ps_log];
-                gone[kb] = id < 0 || id >= p.n_pages;
-                const size_t unit = (size_t)(gone[kb] ? 0 : id) * p.Hkv + g;
-                const size_t off = ((unit << p.ps_log) + (key & ((1 << p.ps_log) - 1))) * HD;
-                st.load(kb, (const typename S::elem *)p.k + off, (const typename S::elem *)p.v + off,
-                        KIND == PAGED_E4M3 ? p.k_scales[unit] : 1.f, KIND == PAGED_E4M3 ? p.v_scales[unit] : 1.f, n, kg);
+                for (int i = 0; i < 4; ++i) st.clear_value(4 * kb + i);
             }
+        }
+        const bool past = k0 + KS > c1, part = k0 + KS > vis_min;
+        if (past)                                // nobody's keys: whatever the page holds there must not meet a weight of 0
 #pragma unroll
-            for (int kb = 0; kb < NKB; ++kb) {
-                if (gone[kb]) {                      // a page that is not there reads as zeros
-                    st.clear_keys(kb);
+            for (int i = 0; i < 4 * NKB; ++i)
+                if (k0 + 16 * (i >> 2) + 4 * kg + (i & 3) >= c1) st.clear_value(i);
+        f32x4 s[NR][NKB];
+        const auto sees = [&](int r, int i) { return k0 + 16 * (i >> 2) + 4 * kg + (i & 3) < min(limit[r], c1); };
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) st.clear_value(4 * kb + i);
+        for (int r = 0; r < NR; ++r) {
+            st.scores(q[r], s[r]);
+            float mx = -INFINITY;
+#pragma unroll
+            for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if ((past || part) && !sees(r, 4 * kb + j)) s[r][kb][j] = -INFINITY;
+                    mx = fmaxf(mx, s[r][kb][j]);
                 }
-            }
-            const bool past = k0 + KS > c1, part = k0 + KS > vis_min;
-            if (past)                                // nobody's keys: whatever the page holds there must not meet a weight of 0
+            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            const float m_new = fmaxf(m_run[r], mx * sl2e);
+            const float m_ref = m_new == -INFINITY ? 0.f : m_new;      // nothing seen yet: every weight is 0
+            const float alpha = pexp2(m_run[r] - m_ref);
+            m_run[r] = m_new;
+            float sum = 0.f;
 #pragma unroll
-                for (int i = 0; i < 4 * NKB; ++i)
-                    if (k0 + 16 * (i >> 2) + 4 * kg + (i & 3) >= c1) st.clear_value(i);
-            f32x4 s[NR][NKB];
-            const auto sees = [&](int r, int i) { return k0 + 16 * (i >> 2) + 4 * kg + (i & 3) < min(limit[r], c1); };
+            for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-            for (int r = 0; r < NR; ++r) {
-                st.scores(q[r], s[r]);
-                float mx = -INFINITY;
+                for (int j = 0; j < 4; ++j) {
+                    s[r][kb][j] = pexp2(fmaf(s[r][kb][j], sl2e, -m_ref));
+                    sum += s[r][kb][j];
+                }
+            l_run[r] = l_run[r] * alpha + sum;
 #pragma unroll
-                for (int kb = 0; kb < NKB; ++kb)
+            for (int i = 0; i < CPL; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if ((past || part) && !sees(r, 4 * kb + j)) s[r][kb][j] = -INFINITY;
-                        mx = fmaxf(mx, s[r][kb][j]);
-                    }
-                mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-                mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-                const float m_new = fmaxf(m_run[r], mx * sl2e);
-                const float m_ref = m_new == -INFINITY ? 0.f : m_new;      // nothing seen yet: every weight is 0
-                const float alpha = pexp2(m_run[r] - m_ref);
-                m_run[r] = m_new;
-                float sum = 0.f;
-#pragma unroll
-                for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        s[r][kb][j] = pexp2(fmaf(s[r][kb][j], sl2e, -m_ref));
-                        sum += s[r][kb][j];
-                    }
-                l_run[r] = l_run[r] * alpha + sum;
-#pragma unroll
-                for (int i = 0; i < CPL; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) o[r][i][j] *= alpha;
-            }
-            const bool odd = part && vis_min != vis_max && __any(st.take_odd());
-            st.template values<NR>(s, o);
-            if (odd)
+                for (int j = 0; j < 4; ++j) o[r][i][j] *= alpha;
+        }
+        const bool odd = part && vis_min != vis_max && __any(st.take_odd());
+        st.template values<NR>(s, o);
+        if (odd)
 #pragma unroll 1
-                for (int key = k0; key < min(k0 + KS, c1); ++key) {
-                    const int id = pages[key >> p.ps_log];
-                    if (id < 0 || id >= p.n_pages) continue;
-                    const size_t unit = (size_t)id * p.Hkv + g;
-                    const typename S::elem *src = (const typename S::elem *)p.v + ((unit << p.ps_log) + (key & ((1 << p.ps_log) - 1))) * HD + 4 * CPL * kg;
-                    const float scale = KIND == PAGED_E4M3 ? p.v_scales[unit] : 1.f;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int i = 0; i < CPL; ++i) {
-                            const float x = S::value(src[CPL * j + i], scale);
-                            if (!(fabsf(x) < INFINITY))
-#pragma unroll
-                                for (int r = 0; r < NR; ++r)
-                                    if (key < limit[r]) o[r][i][j] += x;
-                        }
-                }
-        }
-
-        // ---- join the waves -------------------------------------------------------------------------------------------------
-        const int nw = max(min((c1 - c0 + KS - 1) / KS, kWaves), 1);       // waves that had a step
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            float l = l_run[r] + __shfl_xor(l_run[r], 16, 64);
-            l += __shfl_xor(l, 32, 64);
-            if (wave < nw && 16 * r + n < nrows) {
-                if (kg == 0) {
-                    ml[(wave * R + 16 * r + n) * 2] = m_run[r];
-                    ml[(wave * R + 16 * r + n) * 2 + 1] = l;
-                }
-                float *dst = os + (wave * R + 16 * r + n) * LD + 4 * CPL * kg;
+            for (int key = k0; key < min(k0 + KS, c1); ++key) {
+                const int id = pages[key >> p.ps_log];
+                if (id < 0 || id >= p.n_pages) continue;
+                const size_t unit = (size_t)id * p.Hkv + g;
+                const typename S::elem *src = (const typename S::elem *)p.v + ((unit << p.ps_log) + (key & ((1 << p.ps_log) - 1))) * HD + 4 * CPL * kg;
+                const float scale = KIND == PAGED_E4M3 ? p.v_scales[unit] : 1.f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int d = 0; d < CPL / 4; ++d)
-                        *(f32x4 *)(dst + CPL * j + 4 * d) = f32x4{o[r][4 * d][j], o[r][4 * d + 1][j], o[r][4 * d + 2][j], o[r][4 * d + 3][j]};
-            }
-        }
-        __syncthreads();
-        const int part0 = ((pre_split[b] + u * nc) * p.Hkv) + g * nc_u;    // first partial of the unit
-        for (int e = tid; e < nrows * (HD / 4); e += 256) {
-            const int row = e / (HD / 4), d = (e & (HD / 4 - 1)) * 4;
-            float M = -INFINITY, L = 0.f;
-            for (int i = 0; i < nw; ++i) M = fmaxf(M, ml[(i * R + row) * 2]);
-            f32x4 x = {0.f, 0.f, 0.f, 0.f};
-            for (int i = 0; i < nw; ++i) {
-                const float m = ml[(i * R + row) * 2];
-                const float w = m == -INFINITY ? 0.f : pexp2(m - M);
-                L += w * ml[(i * R + row) * 2 + 1];
-                const f32x4 y = *(const f32x4 *)(os + (i * R + row) * LD + d);
+                    for (int i = 0; i < CPL; ++i) {
+                        const float x = S::value(src[CPL * j + i], scale);
+                        if (!(fabsf(x) < INFINITY))
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] += w * y[j];
+                            for (int r = 0; r < NR; ++r)
+                                if (key < limit[r]) o[r][i][j] += x;
+                    }
             }
-            const int tok = (r0 + row) / a.G, head = g * a.G + r0 + row - tok * a.G;
-            if (nc_u == 1) {
-                const float inv = 1.f / L;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] = before + tok < 0 ? 0.f : x[j] * inv;
-                store4((T *)a.out + ((size_t)(start + tok) * a.Hq + head) * HD + d, x);
-            } else {
-                const size_t at = (size_t)(part0 + c) * R + row;
-                *(f32x4 *)(a.parts.o + at * HD + d) = x;
-                if (d == 0) *(float2 *)(a.parts.ml + at * 2) = make_float2(M, L);
-            }
-        }
-        if (nc > 1 && c == 0 && tid < 8) {
-            const int vals[8] = {part0, nc_u, start, r0, rows * a.G, g, before, 0};
-            int v = vals[0];
-#pragma unroll
-            for (int i = 1; i < 8; ++i) v = tid == i ? vals[i] : v;
-            a.parts.desc[(size_t)((pre_unit[b] + u) * p.Hkv + g) * 8 + tid] = v;
-        }
-        __syncthreads();
     }
+
+    // ---- join the waves -------------------------------------------------------------------------------------------------
+    const int nw = max(min((c1 - c0 + KS - 1) / KS, kWaves), 1);       // waves that had a step
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        float l = l_run[r] + __shfl_xor(l_run[r], 16, 64);
+        l += __shfl_xor(l, 32, 64);
+        if (wave < nw && 16 * r + n < nrows) {
+            if (kg == 0) {
+                ml[(wave * R + 16 * r + n) * 2] = m_run[r];
+                ml[(wave * R + 16 * r + n) * 2 + 1] = l;
+            }
+            float *dst = os + (wave * R + 16 * r + n) * LD + 4 * CPL * kg;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int d = 0; d < CPL / 4; ++d)
+                    *(f32x4 *)(dst + CPL * j + 4 * d) = f32x4{o[r][4 * d][j], o[r][4 * d + 1][j], o[r][4 * d + 2][j], o[r][4 * d + 3][j]};
+        }
+    }
+    __syncthreads();
+    const int part0 = (found.split + u * nc) * p.Hkv + g * nc_u;       // first partial of the unit
+    for (int e = tid; e < nrows * (HD / 4); e += 256) {
+        const int row = e / (HD / 4), d = (e & (HD / 4 - 1)) * 4;
+        float M = -INFINITY, L = 0.f;
+        for (int i = 0; i < nw; ++i) M = fmaxf(M, ml[(i * R + row) * 2]);
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < nw; ++i) {
+            const float m = ml[(i * R + row) * 2];
+            const float w = m == -INFINITY ? 0.f : pexp2(m - M);
+            L += w * ml[(i * R + row) * 2 + 1];
+            const f32x4 y = *(const f32x4 *)(os + (i * R + row) * LD + d);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] += w * y[j];
+        }
+        const int tok = (r0 + row) / a.G, head = g * a.G + r0 + row - tok * a.G;
+        if (nc_u == 1) {
+            const float inv = 1.f / L;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = before + tok < 0 ? 0.f : x[j] * inv;
+            store4((T *)a.out + ((size_t)(start + tok) * a.Hq + head) * HD + d, x);
+        } else {
+            const size_t at = (size_t)(part0 + c) * R + row;
+            *(f32x4 *)(a.parts.o + at * HD + d) = x;
+            if (d == 0) *(float2 *)(a.parts.ml + at * 2) = make_float2(M, L);
+        }
+    }
+    if (nc > 1 && c == 0 && tid == 0)
+        paged_describe(a, (found.unit + u) * p.Hkv + g, part0, nc_u, start, r0, rows * a.G, g, before);
 }
 
 // Adds up the partials of a split unit: o = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c.  A workgroup takes a row at a
-// time, its four waves the row's partials in turn.
+// time, its four waves the row's partials in turn; first the few-row kernel's units, then the other's.
 template <int KIND, int HD>
-__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a)
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a, PagedParts few, PagedParts many)
 {
     typedef typename std::conditional<KIND == PAGED_F32, float, bf16_t>::type T;
     constexpr int CH = HD / 64;
     __shared__ float xs[kWaves][HD], ls[kWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, R = a.parts.rows;
-    const int tasks = a.parts.head[0] * R;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int tasks_few = few.head ? few.head[0] * few.rows : 0, tasks = tasks_few + (many.head ? many.head[0] * many.rows : 0);
     for (int t = blockIdx.x; t < tasks; t += gridDim.x) {
-        const int32_t *desc = a.parts.desc + (size_t)(t / R) * 8;
-        const int part0 = desc[0], nc = desc[1], start = desc[2], r = desc[3] + t % R, rows = desc[4], g = desc[5], before = desc[6];
+        const PagedParts &from = t < tasks_few ? few : many;
+        const int at_task = t < tasks_few ? t : t - tasks_few, R = from.rows, lr = at_task % R;
+        const int32_t *desc = from.desc + (size_t)(at_task / R) * 8;
+        const int part0 = desc[0], nc = desc[1], start = desc[2], r = desc[3] + lr, rows = desc[4], g = desc[5], before = desc[6];
         if (nc == 1 || r >= rows) continue;
         float M = -INFINITY;
-        for (int c = lane; c < nc; c += 64) M = fmaxf(M, a.parts.ml[((size_t)(part0 + c) * R + t % R) * 2]);
+        for (int c = lane; c < nc; c += 64) M = fmaxf(M, from.ml[((size_t)(part0 + c) * R + lr) * 2]);
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
         float x[CH] = {}, L = 0.f;
 #pragma unroll 4
         for (int c = wave; c < nc; c += kWaves) {
-            const size_t at = (size_t)(part0 + c) * R + t % R;
-            const float2 ml = *(const float2 *)(a.parts.ml + at * 2);
+            const size_t at = (size_t)(part0 + c) * R + lr;
+            const float2 ml = *(const float2 *)(from.ml + at * 2);
             const float w = ml.x == -INFINITY ? 0.f : pexp2(ml.x - M);
             L += w * ml.y;
 #pragma unroll
-            for (int i = 0; i < CH; ++i) x[i] += w * a.parts.o[at * HD + CH * lane + i];
+            for (int i = 0; i < CH; ++i) x[i] += w * from.o[at * HD + CH * lane + i];
         }
         __syncthreads();
 #pragma unroll
@@ -631,39 +532,72 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a)
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------------
-constexpr int kChunkMin = 256;      // keys: two steps for each of the four waves
-constexpr int kTarget = 1024;       // items to aim for: two workgroups on each of the 256 CUs, twice over
+constexpr int kFewRows = 32;        // (token, head) rows of a sequence and kv head up to which paged_rows_kernel takes it
 
+static PagedAttnPart plan_part(int rows, int rows_above, int rows_most, int chunk_min, int target, int hd, const PagedView &p, int G, size_t *end)
+{
+    PagedAttnPart r;
+    r.used = true;
+    r.rows = rows; r.rows_above = rows_above; r.rows_most = rows_most; r.chunk_min = chunk_min; r.target = target;
+    r.units = ((int64_t)p.n_rows * G / rows + p.n_seqs) * p.Hkv;
+    const int64_t chunks = (((int64_t)p.width << p.ps_log) + chunk_min - 1) / chunk_min;
+    r.merge = chunks > 1;
+    r.cap_items = r.merge ? (int)std::min<int64_t>(2 * target, r.units * chunks) : 0;
+    r.cap_units = r.merge ? (int)std::min<int64_t>(target, r.units) : 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = *end;
+        *end = (at + bytes + 255) & ~(size_t)255;
+        return at;
+    };
+    r.off_head = take(r.merge ? 4 : 0);
+    r.off_desc = take((size_t)r.cap_units * 32);
+    r.off_ml = take((size_t)r.cap_items * rows * 8);
+    r.off_o = take((size_t)r.cap_items * rows * hd * 4);
+    return r;
+}
+
+// Sequences of up to kFewRows rows are bound by reading their keys, the others by the matrix pipe: one kernel for each kind,
+// and as the host does not know which a call has, both are launched unless every sequence has one row.  fp32 has the first
+// kernel alone.
 PagedAttnPlan paged_attn_plan(int kind, int hd, const PagedView &p, int Hq)
 {
+    const int G = Hq / p.Hkv, most = 0x7fffffff;
     PagedAttnPlan r;
-    const int G = Hq / p.Hkv;
-    r.rows = !p.starts && G <= 16 ? 16 : 32;
-    r.chunk_min = kChunkMin;
-    r.target = kTarget;
-    const int64_t max_len = (int64_t)p.width << p.ps_log;
-    const int64_t units = ((int64_t)p.n_rows * G / r.rows + p.n_seqs) * p.Hkv;
-    const int64_t chunks = (max_len + kChunkMin - 1) / kChunkMin;
-    r.merge = chunks > 1 && units > 0;
-    r.cap_items = r.merge ? (int)std::min<int64_t>(2 * kTarget, units * chunks) : 0;
-    r.cap_units = r.merge ? (int)std::min<int64_t>(kTarget, units) : 0;
-    const size_t al = 255;
-    r.off_desc = 256;
-    r.off_ml = (r.off_desc + (size_t)r.cap_units * 32 + al) & ~al;
-    r.off_o = (r.off_ml + (size_t)r.cap_items * r.rows * 8 + al) & ~al;
-    r.bytes = r.merge ? r.off_o + (size_t)r.cap_items * r.rows * hd * 4 : 0;
+    r.bytes = 0;
+    r.few.used = r.many.used = r.few.merge = r.many.merge = false;
+    const bool one = !p.starts, tiles = kind != PAGED_F32;
+    // 256 keys are two steps for each of the four waves; 1024 items two workgroups on each of 256 CUs, twice over
+    if (!one || !tiles || G <= kFewRows)
+        r.few = plan_part(one && G <= 16 ? 16 : 32, 0, tiles && !one ? kFewRows : most, 256, 1024, hd, p, G, &r.bytes);
+    // 512 keys are eight tiles; 256 items one workgroup on each CU
+    if (tiles && (!one || G > kFewRows)) r.many = plan_part(256, one ? 0 : kFewRows, most, 512, 256, hd, p, G, &r.bytes);
     return r;
+}
+
+static PagedAttnArgs part_args(PagedAttnArgs a, const PagedAttnPart &t, char *ws)
+{
+    a.rows_above = t.rows_above; a.rows_most = t.rows_most; a.chunk_min = t.chunk_min; a.target = t.target;
+    a.parts.head = t.merge ? (int32_t *)(ws + t.off_head) : nullptr;
+    a.parts.desc = (int32_t *)(ws + t.off_desc);
+    a.parts.ml = (float *)(ws + t.off_ml);
+    a.parts.o = (float *)(ws + t.off_o);
+    a.parts.rows = t.rows;
+    return a;
+}
+// items of a call: a chunk more than len / chunk for every unit
+static unsigned part_grid(const PagedAttnPart &t)
+{
+    return (unsigned)(t.units + (t.merge ? t.target : 0));
 }
 
 template <int KIND, int HD, int NR>
 static hipError_t launch_rows(const PagedAttnArgs &a, unsigned grid, hipStream_t s)
 {
-    const size_t lds = (size_t)(kWaves * 16 * NR * (HD + 6) + 3 * (a.p.n_seqs + 1)) * 4;
+    constexpr int lds = kWaves * 16 * NR * (HD + 6) * 4;
     static OncePerDevice attr;
     int dev;
     if (attr.need(&dev)) {
-        const size_t most = (size_t)(kWaves * 16 * NR * (HD + 6) + 3 * (kPagedMaxSeqs + 1)) * 4;
-        hipError_t e = hipFuncSetAttribute((const void *)paged_rows_kernel<KIND, HD, NR>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+        hipError_t e = hipFuncSetAttribute((const void *)paged_rows_kernel<KIND, HD, NR>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (e != hipSuccess) return e;
         attr.mark(dev);
     }
@@ -672,29 +606,24 @@ static hipError_t launch_rows(const PagedAttnArgs &a, unsigned grid, hipStream_t
 }
 
 template <int KIND, int HD>
-static hipError_t launch_kind(const PagedAttnArgs &a, const PagedAttnPlan &plan, hipStream_t s)
+static hipError_t launch_kind(const PagedAttnArgs &a, const PagedAttnPlan &plan, char *ws, hipStream_t s)
 {
-    const int64_t units = ((int64_t)a.p.n_rows * a.G / plan.rows + a.p.n_seqs) * a.p.Hkv;
-    const unsigned grid = (unsigned)std::min<int64_t>(units + (plan.merge ? plan.target : 0), 1 << 20);
-    hipError_t e = plan.rows == 16 ? launch_rows<KIND, HD, 1>(a, grid, s) : launch_rows<KIND, HD, 2>(a, grid, s);
-    if (e != hipSuccess || !plan.merge) return e;
-    paged_merge_kernel<KIND, HD><<<std::min(plan.cap_units * plan.rows, 2048), 256, 0, s>>>(a);
+    const PagedAttnArgs few = part_args(a, plan.few, ws), many = part_args(a, plan.many, ws);
+    hipError_t e = hipSuccess;
+    if (plan.many.used) e = launch_paged_tiles(KIND, HD, many, part_grid(plan.many), s);
+    if (e == hipSuccess && plan.few.used)
+        e = plan.few.rows == 16 ? launch_rows<KIND, HD, 1>(few, part_grid(plan.few), s) : launch_rows<KIND, HD, 2>(few, part_grid(plan.few), s);
+    const int tasks = std::max(plan.few.merge ? plan.few.cap_units * plan.few.rows : 0, plan.many.merge ? plan.many.cap_units * plan.many.rows : 0);
+    if (e != hipSuccess || tasks == 0) return e;
+    paged_merge_kernel<KIND, HD><<<std::min(tasks, 2048), 256, 0, s>>>(a, few.parts, many.parts);
     return hipGetLastError();
 }
 
-hipError_t launch_paged_attention(int kind, int hd, PagedAttnArgs a, const PagedAttnPlan &plan, char *ws, hipStream_t s)
+hipError_t launch_paged_attention(int kind, int hd, const PagedAttnArgs &a, const PagedAttnPlan &plan, char *ws, hipStream_t s)
 {
-    a.chunk_min = plan.chunk_min;
-    a.target = plan.target;
-    a.parts.head = plan.merge ? (int32_t *)ws : nullptr;
-    a.parts.desc = (int32_t *)(ws + plan.off_desc);
-    a.parts.ml = (float *)(ws + plan.off_ml);
-    a.parts.o = (float *)(ws + plan.off_o);
-    a.parts.cap_units = plan.cap_units;
-    a.parts.rows = plan.rows;
-    if (kind == PAGED_BF16) return hd == 128 ? launch_kind<PAGED_BF16, 128>(a, plan, s) : launch_kind<PAGED_BF16, 64>(a, plan, s);
-    if (kind == PAGED_E4M3) return hd == 128 ? launch_kind<PAGED_E4M3, 128>(a, plan, s) : launch_kind<PAGED_E4M3, 64>(a, plan, s);
-    return hd == 128 ? launch_kind<PAGED_F32, 128>(a, plan, s) : launch_kind<PAGED_F32, 64>(a, plan, s);
+    if (kind == PAGED_BF16) return hd == 128 ? launch_kind<PAGED_BF16, 128>(a, plan, ws, s) : launch_kind<PAGED_BF16, 64>(a, plan, ws, s);
+    if (kind == PAGED_E4M3) return hd == 128 ? launch_kind<PAGED_E4M3, 128>(a, plan, ws, s) : launch_kind<PAGED_E4M3, 64>(a, plan, ws, s);
+    return hd == 128 ? launch_kind<PAGED_F32, 128>(a, plan, ws, s) : launch_kind<PAGED_F32, 64>(a, plan, ws, s);
 }
 
 }  // namespace pd
