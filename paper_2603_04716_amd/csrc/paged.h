@@ -20,9 +20,16 @@ struct PagedView {
     int32_t n_seqs, n_rows, width, ps_log, n_pages, Hkv;
 };
 
+// What a kernel only reads, as constant memory: at a wave-uniform index the load is a scalar one, which waits for no vector
+// load that is still under way.
+template <typename T>
+__device__ __forceinline__ T load_const(const T *p, size_t i)
+{
+    return ((const T __attribute__((address_space(4))) *)(uintptr_t)p)[i];
+}
 __device__ __forceinline__ int paged_start(const PagedView &p, int b)
 {
-    return p.starts ? min(max(p.starts[b], 0), p.n_rows) : b;
+    return p.starts ? min(max(load_const(p.starts, b), 0), p.n_rows) : b;
 }
 // rows of sequence b (a host check keeps n_rows >= n_seqs where starts is null)
 __device__ __forceinline__ int paged_rows(const PagedView &p, int b, int start)
@@ -31,7 +38,7 @@ __device__ __forceinline__ int paged_rows(const PagedView &p, int b, int start)
 }
 __device__ __forceinline__ int paged_len(const PagedView &p, int b)
 {
-    return min(max(p.lens[b], 0), p.width << p.ps_log);
+    return min(max(load_const(p.lens, b), 0), p.width << p.ps_log);
 }
 
 struct PagedAppendArgs {
@@ -70,7 +77,7 @@ struct PagedAttnPart {
     bool used, merge;                // launched at all; some of its sequences may be split
     int rows;                        // query rows of a unit
     int rows_above, rows_most, chunk_min, target;
-    int64_t units;                   // at most
+    int64_t units, chunks;           // units of the call and chunks of a sequence: at most
     int cap_units, cap_items;        // split units and their partials: at most
     size_t off_head, off_desc, off_ml, off_o;
 };

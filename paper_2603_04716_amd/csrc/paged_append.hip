@@ -70,13 +70,13 @@ __device__ __forceinline__ void append_rows(const PagedAppendArgs &a, int row0, 
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     if (wave < n) {                                  // a wave finds the sequence, position and page of one row
         const int row = row0 + wave;
-        const int b = p.starts ? wave_last_le(p.n_seqs, row, [&](int i) { return p.starts[i]; }) : min(row, p.n_seqs - 1);
+        const int b = p.starts ? wave_last_le(p.n_seqs, row, [&](int i) { return load_const(p.starts, i); }) : min(row, p.n_seqs - 1);
         const int start = paged_start(p, b), rows = paged_rows(p, b, start);
         const int i = row - start, pos = paged_len(p, b) - rows + i;
         int page = -1;
         const bool held = i >= 0 && i < rows && pos >= 0;
         if (KV && held) {
-            page = p.table[(size_t)b * p.width + (pos >> p.ps_log)];
+            page = load_const(p.table, (size_t)b * p.width + (pos >> p.ps_log));
             if (page >= p.n_pages) page = -1;        // such a position has no page: nothing is stored for it
         }
         if (lane == 0) {
@@ -192,7 +192,7 @@ __global__ __launch_bounds__(256) void paged_append_codes_kernel(PagedAppendArgs
     const int t = (p0 >> ps_log) + pj - ((start >> ps_log) + 2 * b);
     const int lo = max(p0, t << ps_log), hi = min(len, (t + 1) << ps_log);
     if (rows == 0 || t < 0 || lo >= hi) return;
-    const int page = p.table[(size_t)b * p.width + t];
+    const int page = load_const(p.table, (size_t)b * p.width + t);
     if (page < 0 || page >= p.n_pages) return;
     const int slot0 = lo & ((1 << ps_log) - 1), n = hi - lo;
     const int row0 = start + lo - (len - rows);

@@ -311,20 +311,19 @@ __global__ __launch_bounds__(256, KIND == PAGED_F32 ? 1 : 2) void paged_rows_ker
     constexpr int R = 16 * NR, NKB = S::NKB, KS = 16 * NKB, CPL = S::CPL, NQ = S::NQ, LD = HD + 4;
     extern __shared__ __attribute__((aligned(16))) float sm[];
     float *os = sm, *ml = sm + kWaves * R * LD;      // per wave: O [R][LD]; (maximum, sum) [R]
-    __shared__ long red[kWaves];
-    __shared__ PagedFound found;
+    __shared__ PagedShared<256> sh;
     const PagedView &p = a.p;
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, kg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const PagedItems it = paged_divide<R, 256>(a, red);
+    const PagedItems it = paged_divide<R, 256>(a, sh);
     if (blockIdx.x == 0 && tid == 0 && a.parts.head) a.parts.head[0] = it.split_units * p.Hkv;
     const float sl2e = a.scale * 1.4426950408889634f;
 
     const int t = blockIdx.x / p.Hkv, g = blockIdx.x - t * p.Hkv;
     if (t >= it.total) return;
-    paged_find<R>(a, it, t, &found);
-    const int b = __builtin_amdgcn_readfirstlane(found.seq), units = __builtin_amdgcn_readfirstlane(found.units);
-    const int nc = __builtin_amdgcn_readfirstlane(found.chunks), at = __builtin_amdgcn_readfirstlane(found.at);
+    paged_find<R>(a, it, t, &sh.found);
+    const int b = __builtin_amdgcn_readfirstlane(sh.found.seq), units = __builtin_amdgcn_readfirstlane(sh.found.units);
+    const int nc = __builtin_amdgcn_readfirstlane(sh.found.chunks), at = __builtin_amdgcn_readfirstlane(sh.found.at);
     const int start = paged_start(p, b), rows = paged_rows(p, b, start), len = paged_len(p, b);
     // row tiles that read the same keys are neighbours, the one that sees most first
     const int c = at / units, u = units - 1 - (at - c * units);
@@ -361,12 +360,12 @@ __global__ __launch_bounds__(256, KIND == PAGED_F32 ? 1 : 2) void paged_rows_ker
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb) {
             const int key = k0 + 16 * kb, at = min(key, len - 1);
-            const int id = pages[at >> p.ps_log];
+            const int id = load_const(pages, at >> p.ps_log);
             gone[kb] = id < 0 || id >= p.n_pages;
             const size_t unit = (size_t)(gone[kb] ? 0 : id) * p.Hkv + g;
             const size_t off = ((unit << p.ps_log) + (key & ((1 << p.ps_log) - 1))) * HD;
             st.load(kb, (const typename S::elem *)p.k + off, (const typename S::elem *)p.v + off,
-                    KIND == PAGED_E4M3 ? p.k_scales[unit] : 1.f, KIND == PAGED_E4M3 ? p.v_scales[unit] : 1.f, n, kg);
+                    KIND == PAGED_E4M3 ? load_const(p.k_scales, unit) : 1.f, KIND == PAGED_E4M3 ? load_const(p.v_scales, unit) : 1.f, n, kg);
         }
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb) {
@@ -419,11 +418,11 @@ __global__ __launch_bounds__(256, KIND == PAGED_F32 ? 1 : 2) void paged_rows_ker
         if (odd)
 #pragma unroll 1
             for (int key = k0; key < min(k0 + KS, c1); ++key) {
-                const int id = pages[key >> p.ps_log];
+                const int id = load_const(pages, key >> p.ps_log);
                 if (id < 0 || id >= p.n_pages) continue;
                 const size_t unit = (size_t)id * p.Hkv + g;
                 const typename S::elem *src = (const typename S::elem *)p.v + ((unit << p.ps_log) + (key & ((1 << p.ps_log) - 1))) * HD + 4 * CPL * kg;
-                const float scale = KIND == PAGED_E4M3 ? p.v_scales[unit] : 1.f;
+                const float scale = KIND == PAGED_E4M3 ? load_const(p.v_scales, unit) : 1.f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -457,7 +456,7 @@ __global__ __launch_bounds__(256, KIND == PAGED_F32 ? 1 : 2) void paged_rows_ker
         }
     }
     __syncthreads();
-    const int part0 = (found.split + u * nc) * p.Hkv + g * nc_u;       // first partial of the unit
+    const int part0 = (sh.found.split + u * nc) * p.Hkv + g * nc_u;       // first partial of the unit
     for (int e = tid; e < nrows * (HD / 4); e += 256) {
         const int row = e / (HD / 4), d = (e & (HD / 4 - 1)) * 4;
         float M = -INFINITY, L = 0.f;
@@ -484,7 +483,7 @@ __global__ __launch_bounds__(256, KIND == PAGED_F32 ? 1 : 2) void paged_rows_ker
         }
     }
     if (nc > 1 && c == 0 && tid == 0)
-        paged_describe(a, (found.unit + u) * p.Hkv + g, part0, nc_u, start, r0, rows * a.G, g, before);
+        paged_describe(a, (sh.found.unit + u) * p.Hkv + g, part0, nc_u, start, r0, rows * a.G, g, before);
 }
 
 // Adds up the partials of a split unit: o = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c.  A workgroup takes a row at a
@@ -537,12 +536,15 @@ constexpr int kFewRows = 32;        // (token, head) rows of a sequence and kv h
 static PagedAttnPart plan_part(int rows, int rows_above, int rows_most, int chunk_min, int target, int hd, const PagedView &p, int G, size_t *end)
 {
     PagedAttnPart r;
-    r.used = true;
     r.rows = rows; r.rows_above = rows_above; r.rows_most = rows_most; r.chunk_min = chunk_min; r.target = target;
-    r.units = ((int64_t)p.n_rows * G / rows + p.n_seqs) * p.Hkv;
-    const int64_t chunks = (((int64_t)p.width << p.ps_log) + chunk_min - 1) / chunk_min;
-    r.merge = chunks > 1;
-    r.cap_items = r.merge ? (int)std::min<int64_t>(2 * target, r.units * chunks) : 0;
+    // a unit of each sequence may be in part, and no sequence has more rows than rows_most
+    const int64_t all = (int64_t)p.n_rows * G;
+    const int64_t seqs = std::min<int64_t>(p.n_seqs, all / (rows_above + 1));
+    r.units = std::min(all / rows + seqs, seqs * ((rows_most - 1) / rows + 1)) * p.Hkv;
+    r.used = r.units > 0;
+    r.chunks = (((int64_t)p.width << p.ps_log) + chunk_min - 1) / chunk_min;
+    r.merge = r.used && r.chunks > 1;
+    r.cap_items = r.merge ? (int)std::min<int64_t>(2 * target, r.units * r.chunks) : 0;
     r.cap_units = r.merge ? (int)std::min<int64_t>(target, r.units) : 0;
     auto take = [&](size_t bytes) {
         const size_t at = *end;
@@ -584,10 +586,10 @@ static PagedAttnArgs part_args(PagedAttnArgs a, const PagedAttnPart &t, char *ws
     a.parts.rows = t.rows;
     return a;
 }
-// items of a call: a chunk more than len / chunk for every unit
 static unsigned part_grid(const PagedAttnPart &t)
 {
-    return (unsigned)(t.units + (t.merge ? t.target : 0));
+    // items of a call: a chunk more than len / chunk for every unit, and no more than all chunks of all units
+    return (unsigned)std::min(t.units + t.target, t.units * t.chunks);
 }
 
 template <int KIND, int HD, int NR>

@@ -55,30 +55,29 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
     constexpr int LPW = TILE / 1024 / 8;             // bf16: load instructions per wave for each of K and V
     constexpr int RPI = 1024 / (HD * 2);             // ... rows of one
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    __shared__ long red[8];
-    __shared__ PagedFound found;
+    __shared__ PagedShared<512> sh;
     const PagedView &p = a.p;
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const PagedItems it = paged_divide<kTileRows, 512>(a, red);
+    const PagedItems it = paged_divide<kTileRows, 512>(a, sh);
     if (blockIdx.x == 0 && tid == 0 && a.parts.head) a.parts.head[0] = it.split_units * p.Hkv;
     const float sl2e = a.scale * 1.4426950408889634f;
     const int ps_mask = (1 << p.ps_log) - 1;
 
     const int t = blockIdx.x / p.Hkv, g = blockIdx.x - t * p.Hkv;
     if (t >= it.total) return;
-    paged_find<kTileRows>(a, it, t, &found);
-    const int b = __builtin_amdgcn_readfirstlane(found.seq), units = __builtin_amdgcn_readfirstlane(found.units);
-    const int nc = __builtin_amdgcn_readfirstlane(found.chunks), at = __builtin_amdgcn_readfirstlane(found.at);
+    paged_find<kTileRows>(a, it, t, &sh.found);
+    const int b = __builtin_amdgcn_readfirstlane(sh.found.seq), units = __builtin_amdgcn_readfirstlane(sh.found.units);
+    const int nc = __builtin_amdgcn_readfirstlane(sh.found.chunks), at = __builtin_amdgcn_readfirstlane(sh.found.at);
     const int start = paged_start(p, b), rows = paged_rows(p, b, start), len = paged_len(p, b);
     const int c = at / units, u = units - 1 - (at - c * units);     // the tile that sees most keys first
     const int r0 = u * kTileRows, nrows = min(kTileRows, rows * a.G - r0);
     const int before = len - rows;
     const int vis_max = max(before + (r0 + nrows - 1) / a.G + 1, 0);
     const int nc_u = max((vis_max + it.chunk - 1) / it.chunk, 1);
-    const int part0 = (found.split + u * nc) * p.Hkv + g * nc_u;
+    const int part0 = (sh.found.split + u * nc) * p.Hkv + g * nc_u;
     if (tid == 0 && nc > 1 && c == 0)
-        paged_describe(a, (found.unit + u) * p.Hkv + g, part0, nc_u, start, r0, rows * a.G, g, before);
+        paged_describe(a, (sh.found.unit + u) * p.Hkv + g, part0, nc_u, start, r0, rows * a.G, g, before);
     const int c0 = c * it.chunk, c1 = min(vis_max, c0 + it.chunk);
     if (c >= nc_u) return;
 
@@ -112,11 +111,11 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
     // bf16: instruction i of a wave brings rows RPI (8 i + wave) .. of the tile.  Its page number is asked for one tile
     // before its rows are.
     int ids[LPW > 0 ? LPW : 1];
-    auto ask = [&](int j) {
+    auto ask = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < LPW; ++i) ids[i] = pages[min(j * kTileKeys + RPI * (8 * i + wave), len - 1) >> p.ps_log];
+        for (int i = 0; i < LPW; ++i) ids[i] = load_const(pages, min(j * kTileKeys + RPI * (8 * i + wave), len - 1) >> p.ps_log);
     };
-    auto issue = [&](int j, unsigned char *st) {
+    auto issue = [&](int j, unsigned char *st) __attribute__((always_inline)) {
         const int lr = lane / (64 / RPI), slot = lane & (64 / RPI - 1);
 #pragma unroll
         for (int i = 0; i < LPW; ++i) {
@@ -139,14 +138,14 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
     unsigned kc[CW], vc[CW];
     float k_sc = 1.f, v_sc = 1.f;
     const int cr = tid >> 3, cp = tid & 7;
-    auto fetch = [&](int j) {
+    auto fetch = [&](int j) __attribute__((always_inline)) {
         const int key = j * kTileKeys + cr;
-        const int id = pages[__builtin_amdgcn_readfirstlane(min(j * kTileKeys + (wave << 3), len - 1)) >> p.ps_log];
+        const int id = load_const(pages, min(j * kTileKeys + (wave << 3), len - 1) >> p.ps_log);
         const bool there = id >= 0 && id < p.n_pages;
         const size_t unit = (size_t)(there ? id : 0) * p.Hkv + g;
         const size_t off = ((unit << p.ps_log) + (key & ps_mask)) * HD + cp * (HD / 8);
-        k_sc = p.k_scales[unit];
-        v_sc = p.v_scales[unit];
+        k_sc = load_const(p.k_scales, unit);
+        v_sc = load_const(p.v_scales, unit);
         const bool in = there && key < c1;
         if (HD == 128) {
             const u32x4 kw = *(const u32x4 *)((const uint8_t *)p.k + off), vw = *(const u32x4 *)((const uint8_t *)p.v + off);
@@ -170,7 +169,7 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
                      __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false)),
                      __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true))};
     };
-    auto commit = [&](unsigned char *st) {
+    auto commit = [&](unsigned char *st) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < CW / 2; ++i) {
             *(u32x4 *)(st + k_off<HD>(cr, cp * (CW / 2) + i)) = widen4(kc[2 * i], kc[2 * i + 1], k_sc);
@@ -178,10 +177,9 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
         }
     };
 
-    // ---- one tile out of stage STG of the ring ----
-    auto tile = [&](const int j, auto STG) {
-        constexpr int stg = decltype(STG)::value;
-        const unsigned char *st = smem + stg * STAGE;
+    // ---- one tile out of stage st of the ring, while the one for which there is room goes to st_to; PART: some row of the unit
+    // does not see all of its keys ----
+    auto tile = [&](const int j, const unsigned char *st, unsigned char *st_to, auto PART) __attribute__((always_inline)) {
         if (KIND == PAGED_BF16) {
             // Loads retire in order: with at most the requests of the AHEAD - 1 later tiles in flight this wave's part of
             // tile j has landed, after the barrier every wave's, and every wave is done with tile j - 1, whose stage
@@ -191,11 +189,11 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
-            issue(min(j + AHEAD, t_hi - 1), smem + ((stg + AHEAD) % NST) * STAGE);
+            issue(min(j + AHEAD, t_hi - 1), st_to);
             ask(min(j + AHEAD + 1, t_hi - 1));
         } else {
             __syncthreads();                     // tile j is written, and tile j - 1 read
-            commit(smem + ((stg + 1) % NST) * STAGE);
+            commit(st_to);
             fetch(min(j + 2, t_hi - 1));
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -231,7 +229,7 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
         load_v(1);
         __builtin_amdgcn_sched_barrier(0);
         // ---- softmax: p = 2^(s scale log2 e - m) ----
-        const bool part = k0 + kTileKeys > w_min;    // some row does not see all of the tile
+        const bool part = decltype(PART)::value && k0 + kTileKeys > w_min;   // ... and of the wave
         if (part)
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
@@ -281,9 +279,9 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
         // A value that is not finite must not reach a row that does not see it, but 0 * infinity would: in a tile seen in
         // part such values leave the product and are added to the rows that see them one by one.
         bool odd = false;
+        if (part)
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            if (part)
+            for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
                 for (int db = 0; db < NDB; ++db)
 #pragma unroll
@@ -294,10 +292,11 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
                         vf[db][ks][i] = fin;
                     }
 #pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
             for (int db = 0; db < NDB; ++db)
                 o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[db][ks]), pf[ks], o[db], 0, 0, 0);
-        }
-        if (__any(odd))
+        if (decltype(PART)::value && __any(odd))
 #pragma unroll 1
             for (int key = k0; key < min(k0 + kTileKeys, c1); ++key) {
 #pragma unroll
@@ -327,14 +326,22 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
             commit(smem);
             fetch(min(t_lo + 1, t_hi - 1));
         }
-        for (int j = t_lo; j < t_hi; j += NST) {
-            tile(j, std::integral_constant<int, 0>{});
-            if (j + 1 < t_hi) tile(j + 1, std::integral_constant<int, 1>{});
+        // the unit's first row sees keys 0 .. vis_min - 1: the tiles below are seen whole by every row, and their stages are
+        // constants, so that a tile's LDS addresses are registers plus immediates
+        const int t_full = max(t_lo, min(t_hi, (before + r0 / a.G + 1) / kTileKeys));
+        auto full = [&](int j, auto STG) __attribute__((always_inline)) {
+            constexpr int stg = decltype(STG)::value;
+            if (j < t_full) tile(j, smem + stg * STAGE, smem + (stg + AHEAD) % NST * STAGE, std::false_type{});
+        };
+        for (int j = t_lo; j < t_full; j += NST) {
+            full(j, std::integral_constant<int, 0>{});
+            full(j + 1, std::integral_constant<int, 1>{});
             if (NST == 4) {
-                if (j + 2 < t_hi) tile(j + 2, std::integral_constant<int, 2 % NST>{});
-                if (j + 3 < t_hi) tile(j + 3, std::integral_constant<int, 3 % NST>{});
+                full(j + 2, std::integral_constant<int, 2 % NST>{});
+                full(j + 3, std::integral_constant<int, 3 % NST>{});
             }
         }
+        for (int j = t_full; j < t_hi; ++j) tile(j, smem + (j - t_lo) % NST * STAGE, smem + (j - t_lo + AHEAD) % NST * STAGE, std::true_type{});
         // the repeated requests of the last tile: none may outlive the workgroup's LDS
         if (KIND == PAGED_BF16) PD_TILE_VMCNT(0);
     }

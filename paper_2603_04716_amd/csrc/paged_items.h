@@ -7,6 +7,8 @@
 // ones are at most twice the items aimed for.  A thread keeps the counts of its own consecutive sequences and the
 // sum of those before; nothing is stored per sequence.
 #pragma once
+#include <type_traits>
+
 #include "paged.h"
 
 namespace pd {
@@ -25,41 +27,22 @@ struct PagedFound {
     int split, unit;                     // split items and split units ahead of the sequence
 };
 
-template <int NT>
-__device__ __forceinline__ long block_sum(long v, long *red)
+// Sum over the lanes up to this one, by data-parallel moves: a cross-lane step through LDS would take ten times as long, and every
+// workgroup waits for the division before its first load.
+template <typename T>
+__device__ __forceinline__ T wave_scan(T v)
 {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    long s = 0;
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) s += red[w];
-    return s;
-}
-// sum over the threads below this one; the sum over all in *all
-template <int NT>
-__device__ __forceinline__ int block_scan(int v, int *red, int *all)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int inc = v;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int u = __shfl_up(inc, off, 64);
-        if (lane >= off) inc += u;
-    }
-    __syncthreads();
-    if (lane == 63) red[wave] = inc;
-    __syncthreads();
-    int base = 0, sum = 0;
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) {
-        if (w == wave) base = sum;
-        sum += red[w];
-    }
-    *all = sum;
-    return base + inc - v;
+    auto add = [&](auto CTRL, auto ROWS) {
+        const int m = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(CTRL)::value, decltype(ROWS)::value, 0xf, true);
+        v += __builtin_bit_cast(T, m);
+    };
+    add(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});    // one lane up, inside rows of 16
+    add(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    add(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    add(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});    // row 0 to 1, 2 to 3
+    add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});    // lane 31 to rows 2 and 3
+    return v;
 }
 // units of sequence b (none where another kernel has the sequence)
 template <int R>
@@ -72,32 +55,73 @@ __device__ __forceinline__ int paged_chunks(const PagedAttnArgs &a, int b, int c
 {
     return max((paged_len(a.p, b) + chunk - 1) / chunk, 1);
 }
-// by all NT threads; red: NT / 64 longs of LDS
+// LDS of the division
+template <int NT>
+struct PagedShared {
+    float keys[NT / 64], rows[NT / 64];
+    int own[NT / 64], split[NT / 64], unit[NT / 64];
+    PagedFound found;
+};
+// By all NT threads.  Sums that only steer the division are fp32: every workgroup forms them in the same order, and the rows'
+// is exact up to 2^24, which no call has more of.
 template <int R, int NT>
-__device__ __forceinline__ PagedItems paged_divide(const PagedAttnArgs &a, long *red)
+__device__ __forceinline__ PagedItems paged_divide(const PagedAttnArgs &a, PagedShared<NT> &sh)
 {
-    const int n = a.p.n_seqs, per = (n + NT - 1) / NT;
+    const int n = a.p.n_seqs, per = (n + NT - 1) / NT, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     PagedItems r = {64, 0, 0, min((int)threadIdx.x * per, n), 0, 0, 0, 0, 0};
     r.b1 = min(r.b0 + per, n);
-    long keys = 0, rows = 0;
+    float keys = 0.f, rows = 0.f;
     for (int b = r.b0; b < r.b1; ++b) {
-        keys += (long)paged_units<R>(a, b) * paged_len(a.p, b);
-        rows += paged_rows(a.p, b, paged_start(a.p, b));
+        keys += (float)paged_units<R>(a, b) * (float)paged_len(a.p, b);
+        rows += (float)paged_rows(a.p, b, paged_start(a.p, b));
     }
-    keys = block_sum<NT>(keys, red) * a.p.Hkv;
-    rows = block_sum<NT>(rows, red);
-    if (rows > a.p.n_rows) return r;                 // the sequences' rows overlap: no such call, and nothing is done
-    r.chunk = (int)min((max((keys + a.target - 1) / a.target, (long)a.chunk_min) + 63) & ~63l, 1l << 30);
-    int split = 0, unit = 0, all;
+    keys = wave_scan(keys);
+    rows = wave_scan(rows);
+    if (lane == 63) {
+        sh.keys[wave] = keys;
+        sh.rows[wave] = rows;
+    }
+    __syncthreads();
+    keys = rows = 0.f;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+        keys += sh.keys[w];
+        rows += sh.rows[w];
+    }
+    if (rows > (float)a.p.n_rows) return r;          // the sequences' rows overlap: no such call, and nothing is done
+    // (1 + 2^-10: more than the roundings of the sum, so that the bound on the split items holds)
+    const float chunk = keys * (float)a.p.Hkv * (1.0009765625f / (float)a.target);
+    r.chunk = ((int)ceilf(fminf(fmaxf(chunk, (float)a.chunk_min), (float)((1 << 30) - 128))) + 63) & ~63;
+    int own = 0, split = 0, unit = 0;
     for (int b = r.b0; b < r.b1; ++b) {
         const int u = paged_units<R>(a, b), nc = paged_chunks(a, b, r.chunk);
-        r.own += u * nc;
+        own += u * nc;
         split += nc > 1 ? u * nc : 0;
         unit += nc > 1 ? u : 0;
     }
-    r.first = block_scan<NT>(r.own, (int *)red, &r.total);
-    r.split = block_scan<NT>(split, (int *)red, &all);
-    r.unit = block_scan<NT>(unit, (int *)red, &r.split_units);
+    const int own_to = wave_scan(own), split_to = wave_scan(split), unit_to = wave_scan(unit);
+    if (lane == 63) {
+        sh.own[wave] = own_to;
+        sh.split[wave] = split_to;
+        sh.unit[wave] = unit_to;
+    }
+    __syncthreads();
+    r.own = own;
+    r.first = own_to - own;
+    r.split = split_to - split;
+    r.unit = unit_to - unit;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+        if (w < wave) {
+            r.first += sh.own[w];
+            r.split += sh.split[w];
+            r.unit += sh.unit[w];
+        }
+        r.total += sh.own[w];
+        r.split_units += sh.unit[w];
+    }
+    r.total = __builtin_amdgcn_readfirstlane(r.total);
+    r.chunk = __builtin_amdgcn_readfirstlane(r.chunk);
     return r;
 }
 // Item t < it.total, written by the thread that has it; ends with a barrier.
