@@ -324,7 +324,8 @@ __global__ __launch_bounds__(256, KIND == PAGED_F32 ? 1 : 2) void paged_rows_ker
     paged_find<R>(a, it, t, &sh.found);
     const int b = __builtin_amdgcn_readfirstlane(sh.found.seq), units = __builtin_amdgcn_readfirstlane(sh.found.units);
     const int nc = __builtin_amdgcn_readfirstlane(sh.found.chunks), at = __builtin_amdgcn_readfirstlane(sh.found.at);
-    const int start = paged_start(p, b), rows = paged_rows(p, b, start), len = paged_len(p, b);
+    const int start = __builtin_amdgcn_readfirstlane(sh.found.start), rows = __builtin_amdgcn_readfirstlane(sh.found.rows);
+    const int len = __builtin_amdgcn_readfirstlane(sh.found.len);
     // row tiles that read the same keys are neighbours, the one that sees most first
     const int c = at / units, u = units - 1 - (at - c * units);
     const int r0 = u * R, nrows = min(R, rows * a.G - r0);

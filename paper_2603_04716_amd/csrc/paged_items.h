@@ -20,10 +20,11 @@ struct PagedItems {
     int b0, b1;                          // this thread's sequences
     int first, own;                      // items ahead of them, and theirs
     int split, unit;                     // split items and split units ahead of them
+    int start, rows, len;                // the first of them
 };
 struct PagedFound {
     int seq, at;                         // sequence of an item, and the item's place among the sequence's
-    int units, chunks;                   // of the sequence
+    int units, chunks, start, rows, len; // of the sequence
     int split, unit;                     // split items and split units ahead of the sequence
 };
 
@@ -44,16 +45,23 @@ __device__ __forceinline__ T wave_scan(T v)
     add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});    // lane 31 to rows 2 and 3
     return v;
 }
-// units of sequence b (none where another kernel has the sequence)
+// units of a sequence of n rows (none where another kernel has it)
 template <int R>
-__device__ __forceinline__ int paged_units(const PagedAttnArgs &a, int b)
+__device__ __forceinline__ int paged_units(const PagedAttnArgs &a, int n)
 {
-    const int rows = paged_rows(a.p, b, paged_start(a.p, b)) * a.G;
+    const int rows = n * a.G;
     return rows > a.rows_above && rows <= a.rows_most ? (rows + R - 1) / R : 0;
 }
-__device__ __forceinline__ int paged_chunks(const PagedAttnArgs &a, int b, int chunk)
+__device__ __forceinline__ int paged_chunks(int len, int chunk) { return max((len + chunk - 1) / chunk, 1); }
+// f(sequence, first row, rows, positions) for a thread's sequences; the first one's fields are kept, most calls have no more
+template <typename F>
+__device__ __forceinline__ void paged_each(const PagedAttnArgs &a, const PagedItems &r, F f)
 {
-    return max((paged_len(a.p, b) + chunk - 1) / chunk, 1);
+    if (r.b0 < r.b1) f(r.b0, r.start, r.rows, r.len);
+    for (int b = r.b0 + 1; b < r.b1; ++b) {
+        const int start = paged_start(a.p, b);
+        f(b, start, paged_rows(a.p, b, start), paged_len(a.p, b));
+    }
 }
 // LDS of the division
 template <int NT>
@@ -68,13 +76,18 @@ template <int R, int NT>
 __device__ __forceinline__ PagedItems paged_divide(const PagedAttnArgs &a, PagedShared<NT> &sh)
 {
     const int n = a.p.n_seqs, per = (n + NT - 1) / NT, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    PagedItems r = {64, 0, 0, min((int)threadIdx.x * per, n), 0, 0, 0, 0, 0};
+    PagedItems r = {64, 0, 0, min((int)threadIdx.x * per, n), 0, 0, 0, 0, 0, 0, 0, 0};
     r.b1 = min(r.b0 + per, n);
-    float keys = 0.f, rows = 0.f;
-    for (int b = r.b0; b < r.b1; ++b) {
-        keys += (float)paged_units<R>(a, b) * (float)paged_len(a.p, b);
-        rows += (float)paged_rows(a.p, b, paged_start(a.p, b));
+    if (r.b0 < n) {
+        r.start = paged_start(a.p, r.b0);
+        r.rows = paged_rows(a.p, r.b0, r.start);
+        r.len = paged_len(a.p, r.b0);
     }
+    float keys = 0.f, rows = 0.f;
+    paged_each(a, r, [&](int, int, int n_rows, int len) {
+        keys += (float)paged_units<R>(a, n_rows) * (float)len;
+        rows += (float)n_rows;
+    });
     keys = wave_scan(keys);
     rows = wave_scan(rows);
     if (lane == 63) {
@@ -93,12 +106,12 @@ __device__ __forceinline__ PagedItems paged_divide(const PagedAttnArgs &a, Paged
     const float chunk = keys * (float)a.p.Hkv * (1.0009765625f / (float)a.target);
     r.chunk = ((int)ceilf(fminf(fmaxf(chunk, (float)a.chunk_min), (float)((1 << 30) - 128))) + 63) & ~63;
     int own = 0, split = 0, unit = 0;
-    for (int b = r.b0; b < r.b1; ++b) {
-        const int u = paged_units<R>(a, b), nc = paged_chunks(a, b, r.chunk);
+    paged_each(a, r, [&](int, int, int n_rows, int len) {
+        const int u = paged_units<R>(a, n_rows), nc = paged_chunks(len, r.chunk);
         own += u * nc;
         split += nc > 1 ? u * nc : 0;
         unit += nc > 1 ? u : 0;
-    }
+    });
     const int own_to = wave_scan(own), split_to = wave_scan(split), unit_to = wave_scan(unit);
     if (lane == 63) {
         sh.own[wave] = own_to;
@@ -130,16 +143,16 @@ __device__ __forceinline__ void paged_find(const PagedAttnArgs &a, const PagedIt
 {
     if (t >= it.first && t < it.first + it.own) {
         int run = it.first, split = it.split, unit = it.unit;
-        for (int b = it.b0; b < it.b1; ++b) {
-            const int u = paged_units<R>(a, b), nc = paged_chunks(a, b, it.chunk);
-            if (t < run + u * nc) {
+        paged_each(a, it, [&](int b, int start, int rows, int len) {
+            const int u = paged_units<R>(a, rows), nc = paged_chunks(len, it.chunk);
+            if (t >= run && t < run + u * nc) {
                 f->seq = b; f->at = t - run; f->units = u; f->chunks = nc; f->split = split; f->unit = unit;
-                break;
+                f->start = start; f->rows = rows; f->len = len;
             }
             run += u * nc;
             split += nc > 1 ? u * nc : 0;
             unit += nc > 1 ? u : 0;
-        }
+        });
     }
     __syncthreads();
 }
