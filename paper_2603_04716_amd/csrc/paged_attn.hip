@@ -15,6 +15,8 @@
 // channel per lane.  A lane therefore loads hd / 16 channels of its eight keys and swaps halves of registers
 // (v_perm_b32, one per register), which takes no LDS and no lane crossing; accumulator c of a lane is then channel
 // (hd / 16) m + c of the matrix row m, 32 (hd 128) neighbouring channels per lane in all.
+#include <string.h>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -39,6 +41,24 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ unsigned finite_part2(unsigned x)      // of two bf16 values
 {
     return ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u);
+}
+
+// largest value, and sum, over the four lanes of a column (m, m + 16, m + 32, m + 48), in each of them
+__device__ __forceinline__ float across_kg(float x)
+{
+    const unsigned u = __float_as_uint(x);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const unsigned y = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+    const auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum_across_kg(float x)
+{
+    const unsigned u = __float_as_uint(x);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const unsigned y = __float_as_uint(__uint_as_float(a[0]) + __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
 template <typename STEP, int HD>
@@ -102,6 +122,7 @@ struct Step<PAGED_BF16, HD> : Step16<Step<PAGED_BF16, HD>, HD> {
     static constexpr int CPL = HD / 16;
     typedef uint16_t elem;
     u32x4 k[2][HD / 32];
+    bool there[2];
     unsigned v[8][CPL / 2];
     static __device__ __forceinline__ int q_channel(int s, int kg) { return 32 * s + 8 * kg; }
     // kp, vp: rows of the 16-key block kb
@@ -157,6 +178,7 @@ struct Step<PAGED_E4M3, HD> : Step16<Step<PAGED_E4M3, HD>, HD> {
     static constexpr int CPL = HD / 16;
     typedef uint8_t elem;
     u32x4 k[2][HD / 64];
+    bool there[2];
     unsigned v[8][CPL / 4];
     float ks[2], vs[2];
     // 16 consecutive channels per lane and load: k-steps 2 t and 2 t + 1
@@ -225,6 +247,7 @@ struct Step<PAGED_F32, HD> {
     typedef float elem;
     typedef float qfrag;
     f32x4 k[HD / 16], v[4][CPL / 4];
+    bool there[1];
     static __device__ __forceinline__ void load_q(const void *q, int kg, qfrag (&f)[NQ])
     {
 #pragma unroll
@@ -312,251 +335,356 @@ __global__ __launch_bounds__(256, KIND == PAGED_F32 ? 1 : 2) void paged_rows_ker
     extern __shared__ __attribute__((aligned(16))) float sm[];
     float *os = sm, *ml = sm + kWaves * R * LD;      // per wave: O [R][LD]; (maximum, sum) [R]
     __shared__ PagedShared<256> sh;
+    __shared__ PagedPiece piece;
     const PagedView &p = a.p;
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, kg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const PagedItems it = paged_divide<R, 256>(a, sh);
-    if (blockIdx.x == 0 && tid == 0 && a.parts.head) a.parts.head[0] = it.split_units * p.Hkv;
     const float sl2e = a.scale * 1.4426950408889634f;
+    const PagedStream st = paged_stream<R, 256, kWaves * KS>(a, sh);
+    if (a.parts.desc && tid == 0) a.parts.desc[(size_t)blockIdx.x * 8 + 1] = 0;      // no unit of its own to be merged
+    const int end = min((int)(blockIdx.x + 1) * st.per, st.total);
 
-    const int t = blockIdx.x / p.Hkv, g = blockIdx.x - t * p.Hkv;
-    if (t >= it.total) return;
-    paged_find<R>(a, it, t, &sh.found);
-    const int b = __builtin_amdgcn_readfirstlane(sh.found.seq), units = __builtin_amdgcn_readfirstlane(sh.found.units);
-    const int nc = __builtin_amdgcn_readfirstlane(sh.found.chunks), at = __builtin_amdgcn_readfirstlane(sh.found.at);
-    const int start = __builtin_amdgcn_readfirstlane(sh.found.start), rows = __builtin_amdgcn_readfirstlane(sh.found.rows);
-    const int len = __builtin_amdgcn_readfirstlane(sh.found.len);
-    // row tiles that read the same keys are neighbours, the one that sees most first
-    const int c = at / units, u = units - 1 - (at - c * units);
-    const int r0 = u * R, nrows = min(R, rows * a.G - r0);
-    const int before = len - rows;               // position of the sequence's first row (negative: it is not held)
-    const int vis_min = before + r0 / a.G + 1, vis_max = max(before + (r0 + nrows - 1) / a.G + 1, 0);
-    const int nc_u = max((vis_max + it.chunk - 1) / it.chunk, 1);
-    if (c >= nc_u) return;
-    const int c0 = c * it.chunk, c1 = min(vis_max, c0 + it.chunk);
+    for (int at = blockIdx.x * st.per, next; at < end; at = next) {
+        paged_locate<R>(a, st, at, &piece);
+        const int b = __builtin_amdgcn_readfirstlane(piece.seq), start = __builtin_amdgcn_readfirstlane(piece.start);
+        const int rows = __builtin_amdgcn_readfirstlane(piece.rows), len = __builtin_amdgcn_readfirstlane(piece.len);
+        const int nb = __builtin_amdgcn_readfirstlane(piece.blocks), units = __builtin_amdgcn_readfirstlane(piece.units);
+        const int first = __builtin_amdgcn_readfirstlane(piece.before);
+        const int unit = (at - first) / nb, from = at - first - unit * nb;         // the unit, and its first block here
+        const int g = unit / units, u = unit - g * units;
+        const int unit0 = first + unit * nb;                                        // its first block in the stream
+        next = min(unit0 + nb, end);
+        const int r0 = u * R, nrows = min(R, rows * a.G - r0);
+        const int before = len - rows;               // position of the sequence's first row (negative: it is not held)
+        const int vis_min = before + r0 / a.G + 1, vis_max = max(before + (r0 + nrows - 1) / a.G + 1, 0);
+        const int c0 = from * st.gran, c1 = min(vis_max, (next - unit0) * st.gran);   // keys: none where c1 <= c0
+        const int w0 = unit0 / st.per, parts = (unit0 + nb - 1) / st.per - w0 + 1;      // the workgroups that share the unit
 
-    typename S::qfrag q[NR][NQ];
-    int limit[NR];                               // the row sees keys 0 .. limit - 1
-#pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        const int row = r0 + 16 * r + n, tok = row / a.G;
-        const bool ok = row < r0 + nrows;
-        limit[r] = ok ? before + tok + 1 : 0;
-        S::no_q(q[r]);
-        if (ok) S::load_q((const T *)a.q + (start + tok) * a.q_stride + (g * a.G + row - tok * a.G) * HD, kg, q[r]);
-    }
-    f32x4 o[NR][CPL];
-    float m_run[NR], l_run[NR];
-#pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        m_run[r] = -INFINITY;
-        l_run[r] = 0.f;
-#pragma unroll
-        for (int i = 0; i < CPL; ++i) o[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    const int32_t *pages = p.table + (size_t)b * p.width;
-    for (int k0 = c0 + wave * KS; k0 < c1; k0 += kWaves * KS) {
-        S st;
-        bool gone[NKB];
-#pragma unroll
-        for (int kb = 0; kb < NKB; ++kb) {
-            const int key = k0 + 16 * kb, at = min(key, len - 1);
-            const int id = load_const(pages, at >> p.ps_log);
-            gone[kb] = id < 0 || id >= p.n_pages;
-            const size_t unit = (size_t)(gone[kb] ? 0 : id) * p.Hkv + g;
-            const size_t off = ((unit << p.ps_log) + (key & ((1 << p.ps_log) - 1))) * HD;
-            st.load(kb, (const typename S::elem *)p.k + off, (const typename S::elem *)p.v + off,
-                    KIND == PAGED_E4M3 ? load_const(p.k_scales, unit) : 1.f, KIND == PAGED_E4M3 ? load_const(p.v_scales, unit) : 1.f, n, kg);
-        }
-#pragma unroll
-        for (int kb = 0; kb < NKB; ++kb) {
-            if (gone[kb]) {                      // a page that is not there reads as zeros
-                st.clear_keys(kb);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) st.clear_value(4 * kb + i);
-            }
-        }
-        const bool past = k0 + KS > c1, part = k0 + KS > vis_min;
-        if (past)                                // nobody's keys: whatever the page holds there must not meet a weight of 0
-#pragma unroll
-            for (int i = 0; i < 4 * NKB; ++i)
-                if (k0 + 16 * (i >> 2) + 4 * kg + (i & 3) >= c1) st.clear_value(i);
-        f32x4 s[NR][NKB];
-        const auto sees = [&](int r, int i) { return k0 + 16 * (i >> 2) + 4 * kg + (i & 3) < min(limit[r], c1); };
+        typename S::qfrag q[NR][NQ];
+        int limit[NR];                               // the row sees keys 0 .. limit - 1
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-            st.scores(q[r], s[r]);
-            float mx = -INFINITY;
-#pragma unroll
-            for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if ((past || part) && !sees(r, 4 * kb + j)) s[r][kb][j] = -INFINITY;
-                    mx = fmaxf(mx, s[r][kb][j]);
-                }
-            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            const float m_new = fmaxf(m_run[r], mx * sl2e);
-            const float m_ref = m_new == -INFINITY ? 0.f : m_new;      // nothing seen yet: every weight is 0
-            const float alpha = pexp2(m_run[r] - m_ref);
-            m_run[r] = m_new;
-            float sum = 0.f;
-#pragma unroll
-            for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    s[r][kb][j] = pexp2(fmaf(s[r][kb][j], sl2e, -m_ref));
-                    sum += s[r][kb][j];
-                }
-            l_run[r] = l_run[r] * alpha + sum;
-#pragma unroll
-            for (int i = 0; i < CPL; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[r][i][j] *= alpha;
+            const int row = r0 + 16 * r + n, tok = row / a.G;
+            const bool ok = row < r0 + nrows;
+            limit[r] = ok ? before + tok + 1 : 0;
+            S::no_q(q[r]);
+            if (ok) S::load_q((const T *)a.q + (start + tok) * a.q_stride + (g * a.G + row - tok * a.G) * HD, kg, q[r]);
         }
-        const bool odd = part && vis_min != vis_max && __any(st.take_odd());
-        st.template values<NR>(s, o);
-        if (odd)
+        f32x4 o[NR][CPL];
+        float m_run[NR], l_run[NR];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            m_run[r] = -INFINITY;
+            l_run[r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < CPL; ++i) o[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        const int32_t *pages = p.table + (size_t)b * p.width;
+        // Page numbers are asked for a step ahead of the loads, the loads of a step (where the registers hold two of them) a step
+        // ahead of its products.  Past the end the last step is asked for again: after a conditional load the compiler would no
+        // longer know which loads are the older ones, and wait for all.
+        constexpr bool TWO = NR == 1 || KIND == PAGED_F32;
+        const int last = c0 + wave * KS + max(c1 - 1 - c0 - wave * KS, 0) / (kWaves * KS) * (kWaves * KS);     // the wave's last step
+        int ids[NKB];
+        auto ask = [&](int k0) __attribute__((always_inline)) {
+#pragma unroll
+            for (int kb = 0; kb < NKB; ++kb) ids[kb] = load_const(pages, (unsigned)min(min(k0, last) + 16 * kb, len - 1) >> p.ps_log);
+        };
+        auto load = [&](S &st, int k0) __attribute__((always_inline)) {       // the step at k0, whose pages were asked for
+#pragma unroll
+            for (int kb = 0; kb < NKB; ++kb) {
+                const bool there = (unsigned)ids[kb] < (unsigned)p.n_pages;
+                const size_t unit = (size_t)(there ? ids[kb] : 0) * p.Hkv + g;
+                const size_t off = ((unit << p.ps_log) + ((min(k0, last) + 16 * kb) & ((1 << p.ps_log) - 1))) * HD;
+                st.there[kb] = there;
+                st.load(kb, (const typename S::elem *)p.k + off, (const typename S::elem *)p.v + off,
+                        KIND == PAGED_E4M3 ? load_const(p.k_scales, unit) : 1.f, KIND == PAGED_E4M3 ? load_const(p.v_scales, unit) : 1.f, n, kg);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto process = [&](S &st, int k0) __attribute__((always_inline)) {
+#pragma unroll
+            for (int kb = 0; kb < NKB; ++kb)
+                if (!st.there[kb]) {                 // a page that is not there reads as zeros
+                    st.clear_keys(kb);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) st.clear_value(4 * kb + i);
+                }
+            const bool past = k0 + KS > c1, part = k0 + KS > vis_min;
+            if (past)                                // nobody's keys: whatever the page holds there must not meet a weight of 0
+#pragma unroll
+                for (int i = 0; i < 4 * NKB; ++i)
+                    if (k0 + 16 * (i >> 2) + 4 * kg + (i & 3) >= c1) st.clear_value(i);
+            f32x4 s[NR][NKB];
+#pragma unroll
+            for (int r = 0; r < NR; ++r) st.scores(q[r], s[r]);
+            if (past || part)
+#pragma unroll
+                for (int r = 0; r < NR; ++r) {
+                    int seen = min(limit[r], c1) - k0 - 4 * kg;
+                    asm volatile("" : "+v"(seen));   // keeps the branch
+#pragma unroll
+                    for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (16 * kb + j >= seen) s[r][kb][j] = -INFINITY;
+                }
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) mx = fmaxf(mx, s[r][kb][j]);
+                mx = across_kg(mx);
+                const float m_new = fmaxf(m_run[r], mx * sl2e);
+                const float m_ref = m_new == -INFINITY ? 0.f : m_new;      // nothing seen yet: every weight is 0
+                const float alpha = pexp2(m_run[r] - m_ref);
+                m_run[r] = m_new;
+                float sum = 0.f;
+#pragma unroll
+                for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        s[r][kb][j] = pexp2(fmaf(s[r][kb][j], sl2e, -m_ref));
+                        sum += s[r][kb][j];
+                    }
+                l_run[r] = l_run[r] * alpha + sum;
+                if (__any(alpha != 1.f))             // a NaN is not 1 either
+#pragma unroll
+                    for (int i = 0; i < CPL; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) o[r][i][j] *= alpha;
+            }
+            const bool odd = part && vis_min != vis_max && __any(st.take_odd());
+            st.template values<NR>(s, o);
+            if (odd)
 #pragma unroll 1
-            for (int key = k0; key < min(k0 + KS, c1); ++key) {
-                const int id = load_const(pages, key >> p.ps_log);
-                if (id < 0 || id >= p.n_pages) continue;
-                const size_t unit = (size_t)id * p.Hkv + g;
-                const typename S::elem *src = (const typename S::elem *)p.v + ((unit << p.ps_log) + (key & ((1 << p.ps_log) - 1))) * HD + 4 * CPL * kg;
-                const float scale = KIND == PAGED_E4M3 ? load_const(p.v_scales, unit) : 1.f;
+                for (int key = k0; key < min(k0 + KS, c1); ++key) {
+                    const int id = load_const(pages, (unsigned)key >> p.ps_log);
+                    if (id < 0 || id >= p.n_pages) continue;
+                    const size_t unit = (size_t)id * p.Hkv + g;
+                    const typename S::elem *src = (const typename S::elem *)p.v + ((unit << p.ps_log) + (key & ((1 << p.ps_log) - 1))) * HD + 4 * CPL * kg;
+                    const float scale = KIND == PAGED_E4M3 ? load_const(p.v_scales, unit) : 1.f;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int i = 0; i < CPL; ++i) {
+                            const float x = S::value(src[CPL * j + i], scale);
+                            if (!(fabsf(x) < INFINITY))
+#pragma unroll
+                                for (int r = 0; r < NR; ++r)
+                                    if (key < limit[r]) o[r][i][j] += x;
+                        }
+                }
+        };
+        constexpr int D = kWaves * KS;
+        int k0 = c0 + wave * KS;
+        if (k0 < c1) {
+            S sa, sb;
+            ask(k0);
+            if (TWO) {
+                load(sa, k0);
+                ask(k0 + D);
+                for (;; k0 += 2 * D) {
+                    load(sb, k0 + D);
+                    ask(k0 + 2 * D);
+                    process(sa, k0);
+                    if (k0 + D >= c1) break;
+                    load(sa, k0 + 2 * D);
+                    ask(k0 + 3 * D);
+                    process(sb, k0 + D);
+                    if (k0 + 2 * D >= c1) break;
+                }
+            } else {
+                for (; k0 < c1; k0 += D) {
+                    load(sa, k0);
+                    ask(k0 + D);
+                    process(sa, k0);
+                }
+            }
+        }
+
+        // ---- join the waves -------------------------------------------------------------------------------------------------
+        const int nw = max(min((c1 - c0 + KS - 1) / KS, kWaves), 1);       // waves that had a step
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            const float l = sum_across_kg(l_run[r]);
+            if (wave < nw && 16 * r + n < nrows) {
+                if (kg == 0) {
+                    ml[(wave * R + 16 * r + n) * 2] = m_run[r];
+                    ml[(wave * R + 16 * r + n) * 2 + 1] = l;
+                }
+                float *dst = os + (wave * R + 16 * r + n) * LD + 4 * CPL * kg;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int i = 0; i < CPL; ++i) {
-                        const float x = S::value(src[CPL * j + i], scale);
-                        if (!(fabsf(x) < INFINITY))
-#pragma unroll
-                            for (int r = 0; r < NR; ++r)
-                                if (key < limit[r]) o[r][i][j] += x;
-                    }
+                    for (int d = 0; d < CPL / 4; ++d)
+                        *(f32x4 *)(dst + CPL * j + 4 * d) = f32x4{o[r][4 * d][j], o[r][4 * d + 1][j], o[r][4 * d + 2][j], o[r][4 * d + 3][j]};
             }
-    }
-
-    // ---- join the waves -------------------------------------------------------------------------------------------------
-    const int nw = max(min((c1 - c0 + KS - 1) / KS, kWaves), 1);       // waves that had a step
+        }
+        __syncthreads();
+        const int slot = 2 * (int)blockIdx.x + (from == 0);
+        for (int e = tid; e < nrows * (HD / 4); e += 256) {
+            const int row = e / (HD / 4), d = (e & (HD / 4 - 1)) * 4;
+            float M = -INFINITY, L = 0.f;
+            for (int i = 0; i < nw; ++i) M = fmaxf(M, ml[(i * R + row) * 2]);
+            f32x4 x = {0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < nw; ++i) {
+                const float m = ml[(i * R + row) * 2];
+                const float w = m == -INFINITY ? 0.f : pexp2(m - M);
+                L += w * ml[(i * R + row) * 2 + 1];
+                const f32x4 y = *(const f32x4 *)(os + (i * R + row) * LD + d);
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        float l = l_run[r] + __shfl_xor(l_run[r], 16, 64);
-        l += __shfl_xor(l, 32, 64);
-        if (wave < nw && 16 * r + n < nrows) {
-            if (kg == 0) {
-                ml[(wave * R + 16 * r + n) * 2] = m_run[r];
-                ml[(wave * R + 16 * r + n) * 2 + 1] = l;
+                for (int j = 0; j < 4; ++j) x[j] += w * y[j];
             }
-            float *dst = os + (wave * R + 16 * r + n) * LD + 4 * CPL * kg;
+            const int tok = (r0 + row) / a.G, head = g * a.G + r0 + row - tok * a.G;
+            if (parts == 1) {
+                const float inv = 1.f / L;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int d = 0; d < CPL / 4; ++d)
-                    *(f32x4 *)(dst + CPL * j + 4 * d) = f32x4{o[r][4 * d][j], o[r][4 * d + 1][j], o[r][4 * d + 2][j], o[r][4 * d + 3][j]};
+                for (int j = 0; j < 4; ++j) x[j] = before + tok < 0 ? 0.f : x[j] * inv;
+                store4((T *)a.out + ((size_t)(start + tok) * a.Hq + head) * HD + d, x);
+            } else {
+                const size_t to = (size_t)slot * R + row;
+                *(f32x4 *)(a.parts.o + to * HD + d) = x;
+                if (d == 0) *(float2 *)(a.parts.ml + to * 2) = make_float2(M, L);
+            }
         }
+        if (parts > 1 && from == 0 && tid == 0) paged_describe(a, blockIdx.x, 2 * w0 + 1, parts, start, r0, rows * a.G, g, before);
+        __syncthreads();                             // piece, os and ml are read
     }
-    __syncthreads();
-    const int part0 = (sh.found.split + u * nc) * p.Hkv + g * nc_u;       // first partial of the unit
-    for (int e = tid; e < nrows * (HD / 4); e += 256) {
-        const int row = e / (HD / 4), d = (e & (HD / 4 - 1)) * 4;
-        float M = -INFINITY, L = 0.f;
-        for (int i = 0; i < nw; ++i) M = fmaxf(M, ml[(i * R + row) * 2]);
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
-        for (int i = 0; i < nw; ++i) {
-            const float m = ml[(i * R + row) * 2];
-            const float w = m == -INFINITY ? 0.f : pexp2(m - M);
-            L += w * ml[(i * R + row) * 2 + 1];
-            const f32x4 y = *(const f32x4 *)(os + (i * R + row) * LD + d);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] += w * y[j];
-        }
-        const int tok = (r0 + row) / a.G, head = g * a.G + r0 + row - tok * a.G;
-        if (nc_u == 1) {
-            const float inv = 1.f / L;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = before + tok < 0 ? 0.f : x[j] * inv;
-            store4((T *)a.out + ((size_t)(start + tok) * a.Hq + head) * HD + d, x);
-        } else {
-            const size_t at = (size_t)(part0 + c) * R + row;
-            *(f32x4 *)(a.parts.o + at * HD + d) = x;
-            if (d == 0) *(float2 *)(a.parts.ml + at * 2) = make_float2(M, L);
-        }
-    }
-    if (nc > 1 && c == 0 && tid == 0)
-        paged_describe(a, (sh.found.unit + u) * p.Hkv + g, part0, nc_u, start, r0, rows * a.G, g, before);
 }
 
-// Adds up the partials of a split unit: o = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c.  A workgroup takes a row at a
-// time, its four waves the row's partials in turn; first the few-row kernel's units, then the other's.
+// Adds up the partials of split units: o = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i.  hd / 4 threads, four channels each, take
+// a partial of a row.  A wave takes a row of up to kWavePartials partials, a workgroup a row of more (one long sequence).  The
+// tasks run over the units of row 0 first, then of row 1: most units have few rows, and the others' are passed over.
+constexpr int kWavePartials = 8;
+struct MergeTask {
+    const float *ml, *o;                 // of the row's partial 0
+    int64_t rows;                        // rows from partial to partial
+    bool streams;
+    int parts, start, row, g, before;
+};
+template <int HD>
+__device__ __forceinline__ MergeTask merge_task(const PagedParts &few, const PagedParts &many, int units_few, int units_many, int t)
+{
+    const int tasks_few = units_few * few.rows_used;
+    MergeTask k;
+    k.streams = t < tasks_few;
+    const int units = k.streams ? units_few : units_many, at = k.streams ? t : t - tasks_few, rows = k.streams ? few.rows : many.rows;
+    const int lr = at / units;
+    const int32_t *d = (k.streams ? few.desc : many.desc) + (size_t)(at - lr * units) * 8;
+    const int4 lo = *(const int4 *)d, hi = *(const int4 *)(d + 4);
+    const size_t first = (size_t)lo.x * rows + lr;
+    k.ml = (k.streams ? few.ml : many.ml) + first * 2;
+    k.o = (k.streams ? few.o : many.o) + first * HD;
+    k.rows = rows;
+    k.start = lo.z; k.row = lo.w + lr; k.g = hi.y; k.before = hi.z;
+    k.parts = k.row < hi.x ? lo.y : 0;
+    return k;
+}
+// the partials `lane`, lane + step .. of a row, channels 4 d4 ..; M: the row's maximum
+template <int HD>
+__device__ __forceinline__ void merge_sum(const MergeTask &k, int lane, int step, int d4, f32x4 &x, float &L)
+{
+    // partial i: the streams' are slot 2 w + 1 of the first workgroup and slot 2 w of the following ones
+    auto at = [&](int i) { return (k.streams ? max(2 * i - 1, 0) : i) * k.rows; };
+    float M = -INFINITY;
+    for (int i = threadIdx.x & 63; i < k.parts; i += 64) M = fmaxf(M, k.ml[at(i) * 2]);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+    x = f32x4{0.f, 0.f, 0.f, 0.f};
+    L = 0.f;
+#pragma unroll 4
+    for (int i = lane; i < k.parts; i += step) {
+        const float2 f = *(const float2 *)(k.ml + at(i) * 2);
+        const f32x4 y = *(const f32x4 *)(k.o + at(i) * HD + 4 * d4);
+        const float w = f.x == -INFINITY ? 0.f : pexp2(f.x - M);
+        L += w * f.y;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] += w * y[j];
+    }
+}
+template <typename T, int HD>
+__device__ __forceinline__ void merge_store(const PagedAttnArgs &a, const MergeTask &k, int d4, f32x4 x, float L)
+{
+    const int tok = k.row / a.G, head = k.g * a.G + k.row - tok * a.G;
+    const float inv = 1.f / L;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = k.before + tok < 0 ? 0.f : x[j] * inv;
+    store4((T *)a.out + ((size_t)(k.start + tok) * a.Hq + head) * HD + 4 * d4, x);
+}
 template <int KIND, int HD>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a, PagedParts few, PagedParts many)
 {
-    typedef typename std::conditional<KIND == PAGED_F32, float, bf16_t>::type T;
-    constexpr int CH = HD / 64;
-    __shared__ float xs[kWaves][HD], ls[kWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int tasks_few = few.head ? few.head[0] * few.rows : 0, tasks = tasks_few + (many.head ? many.head[0] * many.rows : 0);
-    for (int t = blockIdx.x; t < tasks; t += gridDim.x) {
-        const PagedParts &from = t < tasks_few ? few : many;
-        const int at_task = t < tasks_few ? t : t - tasks_few, R = from.rows, lr = at_task % R;
-        const int32_t *desc = from.desc + (size_t)(at_task / R) * 8;
-        const int part0 = desc[0], nc = desc[1], start = desc[2], r = desc[3] + lr, rows = desc[4], g = desc[5], before = desc[6];
-        if (nc == 1 || r >= rows) continue;
-        float M = -INFINITY;
-        for (int c = lane; c < nc; c += 64) M = fmaxf(M, from.ml[((size_t)(part0 + c) * R + lr) * 2]);
+    typedef typename RowElem<KIND>::type T;
+    constexpr int TPR = HD / 4, NG = 256 / TPR, WG = 64 / TPR;
+    __shared__ f32x4 xs[NG][TPR];
+    __shared__ float ls[NG];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = threadIdx.x / TPR, d4 = threadIdx.x & (TPR - 1);
+    const int units_few = few.desc ? few.units : 0, units_many = many.head ? many.head[0] : 0;
+    const int tasks = units_few * few.rows_used + units_many * many.rows_used;
+    f32x4 x;
+    float L;
+    for (int t = blockIdx.x * 4; t < tasks; t += gridDim.x * 4) {
+        MergeTask k[4];
+        bool any = false;
 #pragma unroll
-        for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
-        float x[CH] = {}, L = 0.f;
-#pragma unroll 4
-        for (int c = wave; c < nc; c += kWaves) {
-            const size_t at = (size_t)(part0 + c) * R + lr;
-            const float2 ml = *(const float2 *)(from.ml + at * 2);
-            const float w = ml.x == -INFINITY ? 0.f : pexp2(ml.x - M);
-            L += w * ml.y;
-#pragma unroll
-            for (int i = 0; i < CH; ++i) x[i] += w * from.o[at * HD + CH * lane + i];
+        for (int i = 0; i < 4; ++i) {
+            k[i] = merge_task<HD>(few, many, units_few, units_many, min(t + i, tasks - 1));
+            if (t + i >= tasks) k[i].parts = 0;
+            any |= k[i].parts > kWavePartials;
         }
-        __syncthreads();
 #pragma unroll
-        for (int i = 0; i < CH; ++i) xs[wave][CH * lane + i] = x[i];
-        if (lane == 0) ls[wave] = L;
-        __syncthreads();
-        const int tok = r / a.G, head = g * a.G + r - tok * a.G;
-        if (threadIdx.x < HD) {
-            const int d = threadIdx.x;
-            const float y = before + tok < 0 ? 0.f : (xs[0][d] + xs[1][d] + xs[2][d] + xs[3][d]) * (1.f / (ls[0] + ls[1] + ls[2] + ls[3]));
-            Elem<T>::st((T *)a.out + ((size_t)(start + tok) * a.Hq + head) * HD + d, y);
-        }
+        for (int i = 0; i < 4; ++i)
+            if (wave == i && k[i].parts > 1 && k[i].parts <= kWavePartials) {
+                merge_sum<HD>(k[i], lane / TPR, WG, d4, x, L);
+#pragma unroll
+                for (int off = TPR; off < 64; off *= 2) {
+                    L += __shfl_xor(L, off, 64);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[j] += __shfl_xor(x[j], off, 64);
+                }
+                if (lane < TPR) merge_store<T, HD>(a, k[i], d4, x, L);
+            }
+        if (!any) continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (k[i].parts > kWavePartials) {
+                merge_sum<HD>(k[i], group, NG, d4, x, L);
+                xs[group][d4] = x;
+                if (d4 == 0) ls[group] = L;
+                __syncthreads();
+                if (group == 0) {
+                    for (int n = 1; n < NG; ++n) {
+                        L += ls[n];
+                        const f32x4 y = xs[n][d4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) x[j] += y[j];
+                    }
+                    merge_store<T, HD>(a, k[i], d4, x, L);
+                }
+                __syncthreads();
+            }
     }
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------------
 constexpr int kFewRows = 32;        // (token, head) rows of a sequence and kv head up to which paged_rows_kernel takes it
+constexpr int kStreams = 512;       // its workgroups: two on each of the 256 CUs
+constexpr int kStreamBlocks = 1;    // fewest blocks (a step for each wave) of one
 
-static PagedAttnPart plan_part(int rows, int rows_above, int rows_most, int chunk_min, int target, int hd, const PagedView &p, int G, size_t *end)
+static size_t take(size_t *end, size_t bytes)
 {
-    PagedAttnPart r;
-    r.rows = rows; r.rows_above = rows_above; r.rows_most = rows_most; r.chunk_min = chunk_min; r.target = target;
-    // a unit of each sequence may be in part, and no sequence has more rows than rows_most
-    const int64_t all = (int64_t)p.n_rows * G;
-    const int64_t seqs = std::min<int64_t>(p.n_seqs, all / (rows_above + 1));
-    r.units = std::min(all / rows + seqs, seqs * ((rows_most - 1) / rows + 1)) * p.Hkv;
-    r.used = r.units > 0;
-    r.chunks = (((int64_t)p.width << p.ps_log) + chunk_min - 1) / chunk_min;
-    r.merge = r.used && r.chunks > 1;
-    r.cap_items = r.merge ? (int)std::min<int64_t>(2 * target, r.units * r.chunks) : 0;
-    r.cap_units = r.merge ? (int)std::min<int64_t>(target, r.units) : 0;
-    auto take = [&](size_t bytes) {
-        const size_t at = *end;
-        *end = (at + bytes + 255) & ~(size_t)255;
-        return at;
-    };
-    r.off_head = take(r.merge ? 4 : 0);
-    r.off_desc = take((size_t)r.cap_units * 32);
-    r.off_ml = take((size_t)r.cap_items * rows * 8);
-    r.off_o = take((size_t)r.cap_items * rows * hd * 4);
-    return r;
+    const size_t at = *end;
+    *end = (at + bytes + 255) & ~(size_t)255;
+    return at;
+}
+// units that a call can have: those of its rows, and a last one in part for each sequence that can have so many rows
+static int64_t most_units(int rows, int rows_above, int rows_most, const PagedView &p, int G)
+{
+    const int64_t all = (int64_t)p.n_rows * G, seqs = std::min<int64_t>(p.n_seqs, all / (rows_above + 1));
+    return std::min(all / rows + seqs, seqs * ((rows_most - 1) / rows + 1)) * p.Hkv;
 }
 
 // Sequences of up to kFewRows rows are bound by reading their keys, the others by the matrix pipe: one kernel for each kind,
@@ -565,32 +693,63 @@ static PagedAttnPart plan_part(int rows, int rows_above, int rows_most, int chun
 PagedAttnPlan paged_attn_plan(int kind, int hd, const PagedView &p, int Hq)
 {
     const int G = Hq / p.Hkv, most = 0x7fffffff;
+    const int64_t max_len = (int64_t)p.width << p.ps_log;
     PagedAttnPlan r;
-    r.bytes = 0;
-    r.few.used = r.many.used = r.few.merge = r.many.merge = false;
+    memset(&r, 0, sizeof(r));
     const bool one = !p.starts, tiles = kind != PAGED_F32;
-    // 256 keys are two steps for each of the four waves; 1024 items two workgroups on each of 256 CUs, twice over
-    if (!one || !tiles || G <= kFewRows)
-        r.few = plan_part(one && G <= 16 ? 16 : 32, 0, tiles && !one ? kFewRows : most, 256, 1024, hd, p, G, &r.bytes);
-    // 512 keys are eight tiles; 256 items one workgroup on each CU
-    if (tiles && (!one || G > kFewRows)) r.many = plan_part(256, one ? 0 : kFewRows, most, 512, 256, hd, p, G, &r.bytes);
+    if (!one || !tiles || G <= kFewRows) {
+        PagedAttnPart &t = r.few;
+        t.rows = one && G <= 16 ? 16 : 32;
+        t.rows_used = one ? std::min(G, t.rows) : t.rows;
+        t.rows_most = tiles && !one ? kFewRows : most;
+        t.least = kStreamBlocks;
+        const int64_t units = most_units(t.rows, 0, t.rows_most, p, G), block = kWaves * (kind == PAGED_F32 ? 16 : 32);
+        const int64_t blocks = (max_len + block - 1) / block;
+        t.grid = (unsigned)std::min<int64_t>(kStreams, units * blocks);
+        t.used = units > 0;
+        t.merge = t.used && blocks > 1 && t.grid > 1;
+        if (t.merge) {
+            t.cap_units = (int)t.grid;
+            t.cap_items = 2 * (int)t.grid;
+        }
+    }
+    if (tiles && (!one || G > kFewRows)) {
+        PagedAttnPart &t = r.many;
+        t.rows = t.rows_used = 256;
+        t.rows_above = one ? 0 : kFewRows;
+        t.rows_most = most;
+        t.least = 512;              // eight tiles
+        t.target = 256;             // a workgroup on each CU
+        const int64_t units = most_units(t.rows, t.rows_above, t.rows_most, p, G), chunks = (max_len + t.least - 1) / t.least;
+        t.used = units > 0;
+        t.grid = (unsigned)std::min(units + t.target, units * chunks);   // a chunk more than len / chunk for every unit
+        t.merge = t.used && chunks > 1;
+        if (t.merge) {
+            t.cap_units = (int)std::min<int64_t>(t.target, units);
+            t.cap_items = (int)std::min<int64_t>(2 * t.target, units * chunks);
+        }
+    }
+    for (PagedAttnPart *t : {&r.few, &r.many}) {
+        t->off_head = take(&r.bytes, t->merge ? 4 : 0);
+        t->off_desc = take(&r.bytes, (size_t)t->cap_units * 32);
+        t->off_ml = take(&r.bytes, (size_t)t->cap_items * t->rows * 8);
+        t->off_o = take(&r.bytes, (size_t)t->cap_items * t->rows * hd * 4);
+    }
     return r;
 }
 
-static PagedAttnArgs part_args(PagedAttnArgs a, const PagedAttnPart &t, char *ws)
+static PagedAttnArgs part_args(PagedAttnArgs a, const PagedAttnPart &t, bool streams, char *ws)
 {
-    a.rows_above = t.rows_above; a.rows_most = t.rows_most; a.chunk_min = t.chunk_min; a.target = t.target;
-    a.parts.head = t.merge ? (int32_t *)(ws + t.off_head) : nullptr;
+    a.rows_above = t.rows_above; a.rows_most = t.rows_most; a.least = t.least; a.target = t.target;
+    if (!t.merge) return a;
+    if (!streams) a.parts.head = (int32_t *)(ws + t.off_head);
     a.parts.desc = (int32_t *)(ws + t.off_desc);
     a.parts.ml = (float *)(ws + t.off_ml);
     a.parts.o = (float *)(ws + t.off_o);
+    a.parts.units = t.cap_units;
     a.parts.rows = t.rows;
+    a.parts.rows_used = t.rows_used;
     return a;
-}
-static unsigned part_grid(const PagedAttnPart &t)
-{
-    // items of a call: a chunk more than len / chunk for every unit, and no more than all chunks of all units
-    return (unsigned)std::min(t.units + t.target, t.units * t.chunks);
 }
 
 template <int KIND, int HD, int NR>
@@ -611,14 +770,14 @@ static hipError_t launch_rows(const PagedAttnArgs &a, unsigned grid, hipStream_t
 template <int KIND, int HD>
 static hipError_t launch_kind(const PagedAttnArgs &a, const PagedAttnPlan &plan, char *ws, hipStream_t s)
 {
-    const PagedAttnArgs few = part_args(a, plan.few, ws), many = part_args(a, plan.many, ws);
+    const PagedAttnArgs few = part_args(a, plan.few, true, ws), many = part_args(a, plan.many, false, ws);
     hipError_t e = hipSuccess;
-    if (plan.many.used) e = launch_paged_tiles(KIND, HD, many, part_grid(plan.many), s);
+    if (plan.many.used) e = launch_paged_tiles(KIND, HD, many, plan.many.grid, s);
     if (e == hipSuccess && plan.few.used)
-        e = plan.few.rows == 16 ? launch_rows<KIND, HD, 1>(few, part_grid(plan.few), s) : launch_rows<KIND, HD, 2>(few, part_grid(plan.few), s);
-    const int tasks = std::max(plan.few.merge ? plan.few.cap_units * plan.few.rows : 0, plan.many.merge ? plan.many.cap_units * plan.many.rows : 0);
+        e = plan.few.rows == 16 ? launch_rows<KIND, HD, 1>(few, plan.few.grid, s) : launch_rows<KIND, HD, 2>(few, plan.few.grid, s);
+    const int tasks = plan.few.cap_units * plan.few.rows_used + plan.many.cap_units * plan.many.rows;
     if (e != hipSuccess || tasks == 0) return e;
-    paged_merge_kernel<KIND, HD><<<std::min(tasks, 2048), 256, 0, s>>>(a, few.parts, many.parts);
+    paged_merge_kernel<KIND, HD><<<std::min((tasks + 3) / 4, 4096), 256, 0, s>>>(a, few.parts, many.parts);
     return hipGetLastError();
 }
 

@@ -104,7 +104,7 @@ __device__ __forceinline__ PagedItems paged_divide(const PagedAttnArgs &a, Paged
     if (rows > (float)a.p.n_rows) return r;          // the sequences' rows overlap: no such call, and nothing is done
     // (1 + 2^-10: more than the roundings of the sum, so that the bound on the split items holds)
     const float chunk = keys * (float)a.p.Hkv * (1.0009765625f / (float)a.target);
-    r.chunk = ((int)ceilf(fminf(fmaxf(chunk, (float)a.chunk_min), (float)((1 << 30) - 128))) + 63) & ~63;
+    r.chunk = ((int)ceilf(fminf(fmaxf(chunk, (float)a.least), (float)((1 << 30) - 128))) + 63) & ~63;
     int own = 0, split = 0, unit = 0;
     paged_each(a, r, [&](int, int, int n_rows, int len) {
         const int u = paged_units<R>(a, n_rows), nc = paged_chunks(len, r.chunk);
@@ -156,6 +156,91 @@ __device__ __forceinline__ void paged_find(const PagedAttnArgs &a, const PagedIt
     }
     __syncthreads();
 }
+
+// ---- the division into equal streams --------------------------------------------------------------------------------------
+//
+// For the kernel that is bound by reading keys: all units' keys in blocks of `gran`, unit after unit (sequence, kv head, row
+// tile), form one stream, and workgroup w of W takes blocks w per .. (w + 1) per - 1 of it, whatever units they belong to.  All
+// workgroups then read the same number of keys, a unit is split only where a border falls into it, and a workgroup has at
+// most two partials: of the unit that it ends (slot 2 w) and of the one that it begins (slot 2 w + 1).
+struct PagedStream {
+    int gran, total, per;                // keys of a block; blocks of the call and of a workgroup
+    int b0, b1, first;                   // this thread's sequences, and the blocks ahead of them
+    int start, rows, len;                // the first of them
+};
+struct PagedPiece {
+    int seq, start, rows, len;           // sequence of a block
+    int before, blocks;                  // blocks ahead of the sequence; blocks of each of its units
+    int units;                           // row tiles (per kv head)
+};
+template <int R, int NT, int BASE>
+__device__ __forceinline__ PagedStream paged_stream(const PagedAttnArgs &a, PagedShared<NT> &sh)
+{
+    const int n = a.p.n_seqs, per = (n + NT - 1) / NT, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    PagedItems r = {};
+    r.b0 = min((int)threadIdx.x * per, n);
+    r.b1 = min(r.b0 + per, n);
+    if (r.b0 < n) {
+        r.start = paged_start(a.p, r.b0);
+        r.rows = paged_rows(a.p, r.b0, r.start);
+        r.len = paged_len(a.p, r.b0);
+    }
+    float blocks = 0.f, rows = 0.f;
+    paged_each(a, r, [&](int, int, int n_rows, int len) {
+        blocks += (float)paged_units<R>(a, n_rows) * (float)((len + BASE - 1) / BASE);
+        rows += (float)n_rows;
+    });
+    blocks = wave_scan(blocks);
+    rows = wave_scan(rows);
+    if (lane == 63) {
+        sh.keys[wave] = blocks;
+        sh.rows[wave] = rows;
+    }
+    __syncthreads();
+    blocks = rows = 0.f;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+        blocks += sh.keys[w];
+        rows += sh.rows[w];
+    }
+    PagedStream st = {BASE, 0, 1, r.b0, r.b1, 0, r.start, r.rows, r.len};
+    if (rows > (float)a.p.n_rows) return st;         // the sequences' rows overlap: no such call, and nothing is done
+    // larger blocks where their number would not fit an int32 (a sequence without keys is a block too, hence the margin)
+    for (float x = blocks * (float)a.p.Hkv; x > (float)(1 << 29); x *= 0.5f) st.gran *= 2;
+    int own = 0;
+    paged_each(a, r, [&](int, int, int n_rows, int len) { own += a.p.Hkv * paged_units<R>(a, n_rows) * paged_chunks(len, st.gran); });
+    const int own_to = wave_scan(own);
+    if (lane == 63) sh.own[wave] = own_to;
+    __syncthreads();
+    st.first = own_to - own;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+        if (w < wave) st.first += sh.own[w];
+        st.total += sh.own[w];
+    }
+    st.total = __builtin_amdgcn_readfirstlane(st.total);
+    st.per = max((st.total + (int)gridDim.x - 1) / (int)gridDim.x, a.least);
+    return st;
+}
+// The sequence that block t < total belongs to, written by the thread that has it; ends with a barrier.
+template <int R>
+__device__ __forceinline__ void paged_locate(const PagedAttnArgs &a, const PagedStream &st, int t, PagedPiece *f)
+{
+    PagedItems r = {};
+    r.b0 = st.b0; r.b1 = st.b1; r.start = st.start; r.rows = st.rows; r.len = st.len;
+    if (t >= st.first) {
+        int run = st.first;
+        paged_each(a, r, [&](int b, int start, int rows, int len) {
+            const int u = paged_units<R>(a, rows), nb = paged_chunks(len, st.gran), n = a.p.Hkv * u * nb;
+            if (t >= run && t < run + n) {
+                f->seq = b; f->start = start; f->rows = rows; f->len = len; f->before = run; f->blocks = nb; f->units = u;
+            }
+            run += n;
+        });
+    }
+    __syncthreads();
+}
+
 __device__ __forceinline__ void paged_describe(const PagedAttnArgs &a, int unit, int part0, int parts, int start, int r0, int rows, int g,
                                                int before)
 {
