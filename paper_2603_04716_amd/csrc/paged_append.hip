@@ -23,13 +23,20 @@ __device__ __forceinline__ int wave_last_le(int n, int x, KEY key)
     return blk + max(__popcll(__ballot(lane < stride && i < n && key(min(i, n - 1)) <= x)) - 1, 0);
 }
 
+// (cos, sin) of a position's angle.  Sine and cosine of x, |x| <= pi/4, by their power series up to x^9 and x^8: the first
+// terms left out are 2e-9 and 2e-8, and with fp32's roundings both are within 1e-7 (the library's functions take twice the
+// instructions, and every head forms the factors again).
 __device__ __forceinline__ float2 rope_turn(double turns, int pos)
 {
     double t = (double)pos * turns;
     t -= rint(t);
-    float2 r;
-    sincosf((float)(t * 6.283185307179586), &r.y, &r.x);
-    return r;
+    const float f = (float)t, q = rintf(4.f * f);
+    const float x = fmaf(4.f, f, -q) * 1.57079637f, x2 = x * x;
+    const float s = fmaf(x * x2, fmaf(x2, fmaf(x2, fmaf(x2, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), x);
+    const float c = fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 1.f / 40320.f, -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
+    const int i = (int)q;                            // quarter turns
+    const float a = i & 1 ? s : c, b = i & 1 ? c : s;
+    return make_float2((i + 1) & 2 ? -a : a, i & 2 ? -b : b);
 }
 
 __device__ __forceinline__ void load8(const uint16_t *p, float (&x)[8])
@@ -147,9 +154,9 @@ __device__ __forceinline__ uint2 codes8(const float (&x)[8], float inv)
 // The codes of the slots before the call's first one, read at the page's old scale, at its new one: value * ratio with
 // ratio = old / new, a power of two below 1, so that only values that become subnormal codes are rounded again.
 template <int HD>
-__device__ __forceinline__ void recode(uint8_t *page, int slots, float ratio)
+__device__ __forceinline__ void recode(uint8_t *page, int slots, float ratio, int first, int step)
 {
-    for (int i = threadIdx.x; i < slots * (HD / 16); i += 256) {
+    for (int i = first; i < slots * (HD / 16); i += step) {
         uint4 w = ((uint4 *)page)[i];
         uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -244,8 +251,8 @@ __global__ __launch_bounds__(256) void paged_append_codes_kernel(PagedAppendArgs
     float v_new = scale_for(fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3])));
     uint8_t *kp = (uint8_t *)p.k + ((unit << ps_log) * HD), *vp = (uint8_t *)p.v + ((unit << ps_log) * HD);
     if (slot0 > 0) {
-        if (k_new > k_old) recode<HD>(kp, slot0, k_old / k_new); else k_new = fmaxf(k_new, k_old);
-        if (v_new > v_old) recode<HD>(vp, slot0, v_old / v_new); else v_new = fmaxf(v_new, v_old);
+        if (k_new > k_old) recode<HD>(kp, slot0, k_old / k_new, tid, 256); else k_new = fmaxf(k_new, k_old);
+        if (v_new > v_old) recode<HD>(vp, slot0, v_old / v_new, tid, 256); else v_new = fmaxf(v_new, v_old);
     }
     if (tid == 0) {
         p.k_scales[unit] = k_new;
@@ -265,6 +272,78 @@ __global__ __launch_bounds__(256) void paged_append_codes_kernel(PagedAppendArgs
     }
 }
 
+// E4M3 pages, one row per sequence: HD / 16 lanes have a head of a row - a query head, or a kv head's key and value - and with it
+// all that the call brings to its page, so that nothing has to be exchanged beyond those lanes.
+template <int HD>
+__global__ __launch_bounds__(256) void paged_append_one_kernel(PagedAppendArgs a)
+{
+    constexpr int HALF = HD / 2, TPR = HD / 16;
+    const PagedView &p = a.p;
+    const int hq = a.q ? a.Hq : 0, heads = hq + p.Hkv;
+    const int64_t group = ((int64_t)blockIdx.x * 256 + threadIdx.x) / TPR;
+    const int row = (int)(group / heads), h = (int)(group - (int64_t)row * heads), c = (threadIdx.x & (TPR - 1)) * 8;
+    if (row >= p.n_seqs) return;
+    const bool isq = h < hq;
+    const int g = isq ? 0 : h - hq;
+    float k[2][8], v[2][8];
+    {
+        const uint16_t *ks = isq ? (const uint16_t *)a.q + row * a.q_stride + h * HD + c : (const uint16_t *)a.k + row * a.k_stride + g * HD + c;
+        load8(ks, k[0]);
+        load8(ks + HALF, k[1]);
+        if (!isq) {
+            const uint16_t *vs = (const uint16_t *)a.v + row * a.v_stride + g * HD + c;
+            load8(vs, v[0]);
+            load8(vs + HALF, v[1]);
+        }
+    }
+    const int pos = paged_len(p, row) - 1;
+    if (pos < 0) return;
+    if (a.rope)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float2 f = rope_turn(a.turns[c + j], pos);
+            rope_pair(k[0][j], k[1][j], f.x, f.y, k[0][j], k[1][j]);
+        }
+    if (isq) {
+        uint16_t *dst = (uint16_t *)a.q_out + row * a.q_out_stride + h * HD + c;
+        store8(dst, k[0]);
+        store8(dst + HALF, k[1]);
+        return;
+    }
+    const int page = load_const(p.table, (size_t)row * p.width + (pos >> p.ps_log)), slot = pos & ((1 << p.ps_log) - 1);
+    if (page < 0 || page >= p.n_pages) return;
+    const size_t unit = (size_t)page * p.Hkv + g;
+    const float k_old = p.k_scales[unit], v_old = p.v_scales[unit];
+    float k_most = 0.f, v_most = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (fabsf(k[i][j]) < INFINITY) k_most = fmaxf(k_most, fabsf(k[i][j]));
+            if (fabsf(v[i][j]) < INFINITY) v_most = fmaxf(v_most, fabsf(v[i][j]));
+        }
+#pragma unroll
+    for (int off = TPR / 2; off > 0; off >>= 1) {
+        k_most = fmaxf(k_most, __shfl_xor(k_most, off, 64));
+        v_most = fmaxf(v_most, __shfl_xor(v_most, off, 64));
+    }
+    float k_new = scale_for(k_most), v_new = scale_for(v_most);
+    uint8_t *kp = (uint8_t *)p.k + ((unit << p.ps_log) * HD), *vp = (uint8_t *)p.v + ((unit << p.ps_log) * HD);
+    if (slot > 0) {
+        if (k_new > k_old) recode<HD>(kp, slot, k_old / k_new, threadIdx.x & (TPR - 1), TPR); else k_new = fmaxf(k_new, k_old);
+        if (v_new > v_old) recode<HD>(vp, slot, v_old / v_new, threadIdx.x & (TPR - 1), TPR); else v_new = fmaxf(v_new, v_old);
+    }
+    if (c == 0) {
+        p.k_scales[unit] = k_new;
+        p.v_scales[unit] = v_new;
+    }
+    const size_t off = (size_t)slot * HD + c;
+    *(uint2 *)(kp + off) = codes8(k[0], 1.f / k_new);
+    *(uint2 *)(kp + off + HALF) = codes8(k[1], 1.f / k_new);
+    *(uint2 *)(vp + off) = codes8(v[0], 1.f / v_new);
+    *(uint2 *)(vp + off + HALF) = codes8(v[1], 1.f / v_new);
+}
+
 template <int HD>
 static void launch_codes(const PagedAppendArgs &a, int page_groups, int per_group, unsigned grid, hipStream_t s)
 {
@@ -280,7 +359,12 @@ hipError_t launch_paged_append(int kind, int hd, const PagedAppendArgs &a, hipSt
     // a workgroup per row while that leaves CUs idle, then four: one search and one set of angles per wave
     const int per_group = a.p.n_rows <= 1024 ? 1 : kRowsPerGroup;
     const unsigned row_groups = (unsigned)((a.p.n_rows + per_group - 1) / per_group);
-    if (kind == PAGED_E4M3) {
+    if (kind == PAGED_E4M3 && !a.p.starts) {
+        const int64_t threads = (int64_t)a.p.n_seqs * ((a.q ? a.Hq : 0) + a.p.Hkv) * (hd / 16);
+        const unsigned grid = (unsigned)((threads + 255) / 256);
+        if (hd == 128) paged_append_one_kernel<128><<<grid, 256, 0, s>>>(a);
+        else paged_append_one_kernel<64><<<grid, 256, 0, s>>>(a);
+    } else if (kind == PAGED_E4M3) {
         const int page_groups = (a.p.n_rows >> a.p.ps_log) + 2 * a.p.n_seqs;
         const unsigned grid = (unsigned)(page_groups * a.p.Hkv) + (a.q ? row_groups : 0u);
         if (hd == 128) launch_codes<128>(a, page_groups, per_group, grid, s);
