@@ -53,15 +53,15 @@ hipError_t launch_paged_append(int kind, int hd, const PagedAppendArgs &a, hipSt
 
 // Partial results of units - tiles of query rows of one sequence and kv head - whose keys are divided over several workgroups,
 // for one attention kernel.
+constexpr int kMergeUnits = 4;           // merge_units: at most
 struct PagedParts {
-    int32_t *head;      // [0]: units that may have been split in this call; null: as many as there are workgroups
     int32_t *desc;      // [..][8]: first partial, partials, first row of the sequence, first (token, head) row of the unit, (token,
                         // head) rows of the sequence, kv head, position of the sequence's first row
     float *ml;          // [..][rows][2] running maximum (log2 domain) and sum
     float *o;           // [..][rows][hd] unnormalised
-    int32_t units;      // where head is null
+    int32_t units;      // workgroups that describe one each
     int32_t rows;       // query rows of a unit
-    int32_t rows_used;  // ... of which no unit has more
+    int32_t merge_groups, merge_units;   // workgroups that share the rows of so many described units
 };
 struct PagedAttnArgs {
     PagedView p;
@@ -71,18 +71,17 @@ struct PagedAttnArgs {
     int32_t Hq, G;                   // G = Hq / Hkv
     float scale;
     int32_t rows_above, rows_most;   // this kernel's sequences: more (token, head) rows than the one, at most the other
-    int32_t least;                   // fewest keys of a chunk (many rows), fewest blocks of a workgroup (few)
-    int32_t target;                  // (unit, chunk) items to aim for (many)
+    int32_t least;                   // fewest blocks (few rows) or tiles (many) of a workgroup
     PagedParts parts;
 };
 // How one of the two kernels is launched, and its part of the workspace: from the host's fields of the call alone.
 struct PagedAttnPart {
     bool used, merge;                // launched at all; some of its units may be split
-    int rows, rows_used;             // query rows of a unit, and of which no unit has more
-    int rows_above, rows_most, least, target;
+    int rows;                        // query rows of a unit
+    int rows_above, rows_most, least, merge_groups, merge_units;
     unsigned grid;
     int cap_units, cap_items;        // units to be merged and their partials: at most
-    size_t off_head, off_desc, off_ml, off_o;
+    size_t off_desc, off_ml, off_o;
 };
 struct PagedAttnPlan {
     PagedAttnPart few, many;

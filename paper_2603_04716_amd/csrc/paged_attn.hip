@@ -3,9 +3,10 @@
 //   o = sum_{j <= p} exp(scale q.k_j - m) v_j / sum_{j <= p} exp(scale q.k_j - m)        p = position of the row
 //
 // For few query rows the floor is reading the visible keys and values once.  A unit is a tile of R = 16 NR (token, head)
-// rows of one sequence and kv head: the whole group's query heads share every byte that is read.  A unit's keys are
-// divided into chunks, one workgroup of four waves each; the waves take the chunk's steps of 16 NKB keys in turn, straight
-// from the pages into matrix operands, with the running maximum and sum of the softmax per row, and join in LDS at the end.
+// rows of one sequence and kv head: the whole group's query heads share every byte that is read.  All units' keys form one
+// stream, which is cut into equal parts, a workgroup of four waves each; the waves take the steps of 16 NKB keys in turn,
+// straight from the pages into matrix operands, with the running maximum and sum of the softmax per row, and join in LDS at the
+// end of each unit.
 //
 //   S^T[key, row] = K[key, :] . Q[row, :]      A = keys as they lie in the page, B = the unit's query rows
 //   O^T[c, row]   = V^T[c, key] . P^T[key, row] A = values transposed in registers, B = the exponentials where the first
@@ -555,65 +556,13 @@ __global__ __launch_bounds__(256, KIND == PAGED_F32 ? 1 : 2) void paged_rows_ker
     }
 }
 
-// Adds up the partials of split units: o = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i.  hd / 4 threads, four channels each, take
-// a partial of a row.  A wave takes a row of up to kWavePartials partials, a workgroup a row of more (one long sequence).  The
-// tasks run over the units of row 0 first, then of row 1: most units have few rows, and the others' are passed over.
-constexpr int kWavePartials = 8;
-struct MergeTask {
-    const float *ml, *o;                 // of the row's partial 0
-    int64_t rows;                        // rows from partial to partial
-    bool streams;
-    int parts, start, row, g, before;
-};
-template <int HD>
-__device__ __forceinline__ MergeTask merge_task(const PagedParts &few, const PagedParts &many, int units_few, int units_many, int t)
-{
-    const int tasks_few = units_few * few.rows_used;
-    MergeTask k;
-    k.streams = t < tasks_few;
-    const int units = k.streams ? units_few : units_many, at = k.streams ? t : t - tasks_few, rows = k.streams ? few.rows : many.rows;
-    const int lr = at / units;
-    const int32_t *d = (k.streams ? few.desc : many.desc) + (size_t)(at - lr * units) * 8;
-    const int4 lo = *(const int4 *)d, hi = *(const int4 *)(d + 4);
-    const size_t first = (size_t)lo.x * rows + lr;
-    k.ml = (k.streams ? few.ml : many.ml) + first * 2;
-    k.o = (k.streams ? few.o : many.o) + first * HD;
-    k.rows = rows;
-    k.start = lo.z; k.row = lo.w + lr; k.g = hi.y; k.before = hi.z;
-    k.parts = k.row < hi.x ? lo.y : 0;
-    return k;
-}
-// the partials `lane`, lane + step .. of a row, channels 4 d4 ..; M: the row's maximum
-template <int HD>
-__device__ __forceinline__ void merge_sum(const MergeTask &k, int lane, int step, int d4, f32x4 &x, float &L)
-{
-    // partial i: the streams' are slot 2 w + 1 of the first workgroup and slot 2 w of the following ones
-    auto at = [&](int i) { return (k.streams ? max(2 * i - 1, 0) : i) * k.rows; };
-    float M = -INFINITY;
-    for (int i = threadIdx.x & 63; i < k.parts; i += 64) M = fmaxf(M, k.ml[at(i) * 2]);
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
-    x = f32x4{0.f, 0.f, 0.f, 0.f};
-    L = 0.f;
-#pragma unroll 4
-    for (int i = lane; i < k.parts; i += step) {
-        const float2 f = *(const float2 *)(k.ml + at(i) * 2);
-        const f32x4 y = *(const f32x4 *)(k.o + at(i) * HD + 4 * d4);
-        const float w = f.x == -INFINITY ? 0.f : pexp2(f.x - M);
-        L += w * f.y;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] += w * y[j];
-    }
-}
-template <typename T, int HD>
-__device__ __forceinline__ void merge_store(const PagedAttnArgs &a, const MergeTask &k, int d4, f32x4 x, float L)
-{
-    const int tok = k.row / a.G, head = k.g * a.G + k.row - tok * a.G;
-    const float inv = 1.f / L;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = k.before + tok < 0 ? 0.f : x[j] * inv;
-    store4((T *)a.out + ((size_t)(k.start + tok) * a.Hq + head) * HD + 4 * d4, x);
-}
+// Adds up the partials of split units: o = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i.  `groups` workgroups share the rows of merge_units
+// descriptions, most of which name no split unit.  hd / 4 threads, four channels each, take a partial of a row.  Of up to
+// kWavePartials partials a wave takes four rows together, whose loads are under way at the same time; of more (one long sequence)
+// the workgroup takes one row.
+constexpr int kWavePartials = 16;
+// partial i of a unit: slot 2 w + 1 of the first workgroup, slot 2 w of the following ones
+__device__ __forceinline__ int merge_at(int i) { return max(2 * i - 1, 0); }
 template <int KIND, int HD>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a, PagedParts few, PagedParts many)
 {
@@ -622,56 +571,106 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a, Paged
     __shared__ f32x4 xs[NG][TPR];
     __shared__ float ls[NG];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = threadIdx.x / TPR, d4 = threadIdx.x & (TPR - 1);
-    const int units_few = few.desc ? few.units : 0, units_many = many.head ? many.head[0] : 0;
-    const int tasks = units_few * few.rows_used + units_many * many.rows_used;
-    f32x4 x;
-    float L;
-    for (int t = blockIdx.x * 4; t < tasks; t += gridDim.x * 4) {
-        MergeTask k[4];
-        bool any = false;
+    const int blocks_few = few.units ? (few.units + few.merge_units - 1) / few.merge_units * few.merge_groups : 0;
+    const bool is_few = (int)blockIdx.x < blocks_few;
+    const int block = is_few ? blockIdx.x : blockIdx.x - blocks_few, groups = is_few ? few.merge_groups : many.merge_groups;
+    const int units = is_few ? few.units : many.units, most = is_few ? few.merge_units : many.merge_units, unit = block / groups * most;
+    const int64_t stride = is_few ? few.rows : many.rows;
+    const int32_t *d = is_few ? few.desc : many.desc;
+    const float *ml0 = is_few ? few.ml : many.ml, *o0 = is_few ? few.o : many.o;
+    int4 lo[kMergeUnits], hi[kMergeUnits];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            k[i] = merge_task<HD>(few, many, units_few, units_many, min(t + i, tasks - 1));
-            if (t + i >= tasks) k[i].parts = 0;
-            any |= k[i].parts > kWavePartials;
-        }
+    for (int i = 0; i < kMergeUnits; ++i) {
+        const int32_t *di = d + (size_t)min(unit + i, units - 1) * 8;
+        lo[i] = *(const int4 *)di;
+        hi[i] = *(const int4 *)(di + 4);
+    }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (wave == i && k[i].parts > 1 && k[i].parts <= kWavePartials) {
-                merge_sum<HD>(k[i], lane / TPR, WG, d4, x, L);
+    for (int i = 0; i < kMergeUnits; ++i) {
+        const int parts = lo[i].y, rows = min(hi[i].x - lo[i].w, (int)stride), g = hi[i].y, before = hi[i].z;
+        if (i >= most || unit + i >= units || parts <= 1) continue;
+        const float *ml = ml0 + (size_t)lo[i].x * stride * 2, *o = o0 + (size_t)lo[i].x * stride * HD + 4 * d4;
+        auto store = [&](int r, f32x4 x, float L) {
+            const int row = lo[i].w + r, tok = row / a.G, head = g * a.G + row - tok * a.G;
+            const float inv = 1.f / L;
 #pragma unroll
-                for (int off = TPR; off < 64; off *= 2) {
-                    L += __shfl_xor(L, off, 64);
+            for (int j = 0; j < 4; ++j) x[j] = before + tok < 0 ? 0.f : x[j] * inv;
+            store4((T *)a.out + ((size_t)(lo[i].z + tok) * a.Hq + head) * HD + 4 * d4, x);
+        };
+        if (parts <= kWavePartials) {
+            for (int r = 16 * (block % groups) + 4 * wave; r < rows; r += 16 * groups) {
+                // 16 lanes have a row's weights
+                const int wr = min(r + (lane >> 4), rows - 1), wp = lane & 15;
+                const float2 f = *(const float2 *)(ml + (merge_at(min(wp, parts - 1)) * stride + wr) * 2);
+                float M = f.x;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x[j] += __shfl_xor(x[j], off, 64);
-                }
-                if (lane < TPR) merge_store<T, HD>(a, k[i], d4, x, L);
-            }
-        if (!any) continue;
+                for (int off = 8; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+                const float w = wp < parts && f.x != -INFINITY ? pexp2(f.x - M) : 0.f;
+                float L = w * f.y;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (k[i].parts > kWavePartials) {
-                merge_sum<HD>(k[i], group, NG, d4, x, L);
-                xs[group][d4] = x;
-                if (d4 == 0) ls[group] = L;
-                __syncthreads();
-                if (group == 0) {
-                    for (int n = 1; n < NG; ++n) {
-                        L += ls[n];
-                        const f32x4 y = xs[n][d4];
+                for (int off = 8; off > 0; off >>= 1) L += __shfl_xor(L, off, 64);
+                f32x4 x[4] = {};
+                for (int p = 0; p < parts; p += WG) {
+                    const int mine = p + lane / TPR;
+                    const float *op = o + merge_at(min(mine, parts - 1)) * stride * HD;
+                    f32x4 y[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) x[j] += y[j];
+                    for (int q = 0; q < 4; ++q) y[q] = *(const f32x4 *)(op + (size_t)min(r + q, rows - 1) * HD);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float wq = __shfl(w, 16 * q + (mine & 15), 64);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) x[q][j] += wq * y[q][j];
                     }
-                    merge_store<T, HD>(a, k[i], d4, x, L);
                 }
-                __syncthreads();
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+#pragma unroll
+                    for (int off = TPR; off < 64; off *= 2)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) x[q][j] += __shfl_xor(x[q][j], off, 64);
+                    const float Lq = __shfl(L, 16 * q, 64);
+                    if (r + q < rows && lane < TPR) store(r + q, x[q], Lq);
+                }
             }
+            continue;
+        }
+        for (int r = block % groups; r < rows; r += groups) {
+            float M = -INFINITY, L = 0.f;
+            for (int p = lane; p < parts; p += 64) M = fmaxf(M, ml[(merge_at(p) * stride + r) * 2]);
+#pragma unroll
+            for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+            f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+            for (int p = group; p < parts; p += NG) {
+                const float2 f = *(const float2 *)(ml + (merge_at(p) * stride + r) * 2);
+                const f32x4 y = *(const f32x4 *)(o + (merge_at(p) * stride + r) * HD);
+                const float w = f.x == -INFINITY ? 0.f : pexp2(f.x - M);
+                L += w * f.y;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] += w * y[j];
+            }
+            xs[group][d4] = x;
+            if (d4 == 0) ls[group] = L;
+            __syncthreads();
+            if (group == 0) {
+                for (int n = 1; n < NG; ++n) {
+                    L += ls[n];
+                    const f32x4 y = xs[n][d4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[j] += y[j];
+                }
+                store(r, x, L);
+            }
+            __syncthreads();
+        }
     }
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------------
 constexpr int kFewRows = 32;        // (token, head) rows of a sequence and kv head up to which paged_rows_kernel takes it
 constexpr int kStreams = 512;       // its workgroups: two on each of the 256 CUs
+constexpr int kTileStreams = 256;   // workgroups of the other kernel: one on each
 constexpr int kStreamBlocks = 1;    // fewest blocks (a step for each wave) of one
 
 static size_t take(size_t *end, size_t bytes)
@@ -700,7 +699,6 @@ PagedAttnPlan paged_attn_plan(int kind, int hd, const PagedView &p, int Hq)
     if (!one || !tiles || G <= kFewRows) {
         PagedAttnPart &t = r.few;
         t.rows = one && G <= 16 ? 16 : 32;
-        t.rows_used = one ? std::min(G, t.rows) : t.rows;
         t.rows_most = tiles && !one ? kFewRows : most;
         t.least = kStreamBlocks;
         const int64_t units = most_units(t.rows, 0, t.rows_most, p, G), block = kWaves * (kind == PAGED_F32 ? 16 : 32);
@@ -711,26 +709,28 @@ PagedAttnPlan paged_attn_plan(int kind, int hd, const PagedView &p, int Hq)
         if (t.merge) {
             t.cap_units = (int)t.grid;
             t.cap_items = 2 * (int)t.grid;
+            t.merge_groups = std::min(one ? std::min(G, t.rows) : t.rows, 8);
+            t.merge_units = kMergeUnits;
         }
     }
     if (tiles && (!one || G > kFewRows)) {
         PagedAttnPart &t = r.many;
-        t.rows = t.rows_used = 256;
+        t.rows = 256;
         t.rows_above = one ? 0 : kFewRows;
         t.rows_most = most;
-        t.least = 512;              // eight tiles
-        t.target = 256;             // a workgroup on each CU
-        const int64_t units = most_units(t.rows, t.rows_above, t.rows_most, p, G), chunks = (max_len + t.least - 1) / t.least;
+        t.least = 8;
+        const int64_t units = most_units(t.rows, t.rows_above, t.rows_most, p, G), parts = (max_len + 511) / 512;
+        t.grid = (unsigned)std::min<int64_t>(kTileStreams, units * std::max<int64_t>(parts, 1));
         t.used = units > 0;
-        t.grid = (unsigned)std::min(units + t.target, units * chunks);   // a chunk more than len / chunk for every unit
-        t.merge = t.used && chunks > 1;
+        t.merge = t.used && max_len > 448 && t.grid > 1;        // (a unit of fewer than eight tiles is never split)
         if (t.merge) {
-            t.cap_units = (int)std::min<int64_t>(t.target, units);
-            t.cap_items = (int)std::min<int64_t>(2 * t.target, units * chunks);
+            t.cap_units = (int)t.grid;
+            t.cap_items = 2 * (int)t.grid;
+            t.merge_groups = 16;
+            t.merge_units = 2;
         }
     }
     for (PagedAttnPart *t : {&r.few, &r.many}) {
-        t->off_head = take(&r.bytes, t->merge ? 4 : 0);
         t->off_desc = take(&r.bytes, (size_t)t->cap_units * 32);
         t->off_ml = take(&r.bytes, (size_t)t->cap_items * t->rows * 8);
         t->off_o = take(&r.bytes, (size_t)t->cap_items * t->rows * hd * 4);
@@ -738,17 +738,17 @@ PagedAttnPlan paged_attn_plan(int kind, int hd, const PagedView &p, int Hq)
     return r;
 }
 
-static PagedAttnArgs part_args(PagedAttnArgs a, const PagedAttnPart &t, bool streams, char *ws)
+static PagedAttnArgs part_args(PagedAttnArgs a, const PagedAttnPart &t, char *ws)
 {
-    a.rows_above = t.rows_above; a.rows_most = t.rows_most; a.least = t.least; a.target = t.target;
+    a.rows_above = t.rows_above; a.rows_most = t.rows_most; a.least = t.least;
     if (!t.merge) return a;
-    if (!streams) a.parts.head = (int32_t *)(ws + t.off_head);
     a.parts.desc = (int32_t *)(ws + t.off_desc);
     a.parts.ml = (float *)(ws + t.off_ml);
     a.parts.o = (float *)(ws + t.off_o);
     a.parts.units = t.cap_units;
     a.parts.rows = t.rows;
-    a.parts.rows_used = t.rows_used;
+    a.parts.merge_groups = t.merge_groups;
+    a.parts.merge_units = t.merge_units;
     return a;
 }
 
@@ -770,14 +770,15 @@ static hipError_t launch_rows(const PagedAttnArgs &a, unsigned grid, hipStream_t
 template <int KIND, int HD>
 static hipError_t launch_kind(const PagedAttnArgs &a, const PagedAttnPlan &plan, char *ws, hipStream_t s)
 {
-    const PagedAttnArgs few = part_args(a, plan.few, true, ws), many = part_args(a, plan.many, false, ws);
+    const PagedAttnArgs few = part_args(a, plan.few, ws), many = part_args(a, plan.many, ws);
     hipError_t e = hipSuccess;
     if (plan.many.used) e = launch_paged_tiles(KIND, HD, many, plan.many.grid, s);
     if (e == hipSuccess && plan.few.used)
         e = plan.few.rows == 16 ? launch_rows<KIND, HD, 1>(few, plan.few.grid, s) : launch_rows<KIND, HD, 2>(few, plan.few.grid, s);
-    const int tasks = plan.few.cap_units * plan.few.rows_used + plan.many.cap_units * plan.many.rows;
-    if (e != hipSuccess || tasks == 0) return e;
-    paged_merge_kernel<KIND, HD><<<std::min((tasks + 3) / 4, 4096), 256, 0, s>>>(a, few.parts, many.parts);
+    auto merge_blocks = [](const PagedParts &p) { return p.units ? (p.units + p.merge_units - 1) / p.merge_units * p.merge_groups : 0; };
+    const int blocks = merge_blocks(few.parts) + merge_blocks(many.parts);
+    if (e != hipSuccess || blocks == 0) return e;
+    paged_merge_kernel<KIND, HD><<<blocks, 256, 0, s>>>(a, few.parts, many.parts);
     return hipGetLastError();
 }
 

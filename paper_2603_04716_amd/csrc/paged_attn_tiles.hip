@@ -47,6 +47,34 @@ __device__ __forceinline__ int k_off(int r, int c) { return r * HD * 2 + (HD == 
 template <int HD>
 __device__ __forceinline__ int v_off(int r, int c) { return r * HD * 2 + (HD == 128 ? c ^ ((r & 3) << 2) : c ^ (((r >> 1) & 1) << 2)) * 16; }
 
+// x[i] of lane n + 32 h: piece 2 i + h (16 bytes) of row n.  Afterwards x[4 k + i] of a lane: piece 8 k + rows_piece() of row 8 i + lane % 8,
+// so that a store or load covers eight rows' whole cache lines: 32 rows at 32 bytes each took four times as long.  Its own inverse.
+__device__ __forceinline__ int rows_piece(int lane) { return ((lane & 8) >> 1) + ((lane & 16) >> 3) + (lane >> 5); }
+template <int N>
+__device__ __forceinline__ void rows_swap16(u32x4 (&x)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; i += 2)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const auto s = __builtin_amdgcn_permlane16_swap(x[i][e], x[i + 1][e], false, false);
+            x[i][e] = s[0];
+            x[i + 1][e] = s[1];
+        }
+}
+template <int N>
+__device__ __forceinline__ void rows_swap8(u32x4 (&x)[N])      // lanes 8 .. 15 of each 16 of x[i] with lanes 0 .. 7 of x[i + 2]
+{
+#pragma unroll
+    for (int i = 0; i < N; i += i & 1 ? 3 : 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int lo = x[i][e], hi = x[i + 2][e];
+            x[i][e] = __builtin_amdgcn_update_dpp(lo, hi, 0x128, 0xf, 0xc, false);       // row_ror:8
+            x[i + 2][e] = __builtin_amdgcn_update_dpp(hi, lo, 0x128, 0xf, 0x3, false);
+        }
+}
+
 template <int KIND, int HD>
 __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
 {
@@ -56,67 +84,122 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
     constexpr int LPW = TILE / 1024 / 8;             // bf16: load instructions per wave for each of K and V
     constexpr int RPI = 1024 / (HD * 2);             // ... rows of one
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    __shared__ PagedShared<512> sh;
-    __shared__ int again;
+    __shared__ PagedTilesShared<512> sh;
+    __shared__ unsigned bad;                         // listed units with results that are not finite
     const PagedView &p = a.p;
     const int tid = threadIdx.x, lane = tid & 63;
     int n = lane & 31, h = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const PagedItems it = paged_divide<kTileRows, 512>(a, sh);
-    if (blockIdx.x == 0 && tid == 0 && a.parts.head) a.parts.head[0] = it.split_units * p.Hkv;
-    const float sl2e = a.scale * 1.4426950408889634f;
-    const int ps_mask = (1 << p.ps_log) - 1;
-
-    const int t = blockIdx.x / p.Hkv, g = blockIdx.x - t * p.Hkv;
-    if (t >= it.total) return;
-    paged_find<kTileRows>(a, it, t, &sh.found);
-    const int b = __builtin_amdgcn_readfirstlane(sh.found.seq), units = __builtin_amdgcn_readfirstlane(sh.found.units);
-    const int nc = __builtin_amdgcn_readfirstlane(sh.found.chunks), at = __builtin_amdgcn_readfirstlane(sh.found.at);
-    const int start = __builtin_amdgcn_readfirstlane(sh.found.start), rows = __builtin_amdgcn_readfirstlane(sh.found.rows);
-    const int len = __builtin_amdgcn_readfirstlane(sh.found.len);
-    const int c = at / units, u = units - 1 - (at - c * units);     // the tile that sees most keys first
-    const int r0 = u * kTileRows, nrows = min(kTileRows, rows * a.G - r0);
-    const int before = len - rows;
-    const int vis_max = max(before + (r0 + nrows - 1) / a.G + 1, 0);
-    const int nc_u = max((vis_max + it.chunk - 1) / it.chunk, 1);
-    const int part0 = (sh.found.split + u * nc) * p.Hkv + g * nc_u;
-    if (tid == 0 && nc > 1 && c == 0)
-        paged_describe(a, (sh.found.unit + u) * p.Hkv + g, part0, nc_u, start, r0, rows * a.G, g, before);
-    const int c0 = c * it.chunk, c1 = min(vis_max, c0 + it.chunk);
-    if (c >= nc_u) return;
-
-    // ---- the wave's rows
-    const int w0 = wave * 32, row = r0 + w0 + n, tok = row / a.G;
-    const bool ok = w0 + n < nrows;
-    const int limit = ok ? before + tok + 1 : 0;                    // the row sees keys 0 .. limit - 1
-    const int w_min = before + (r0 + w0) / a.G + 1;                     // ... and the wave's first row 0 .. w_min - 1
-    bf16x8 qf[NK];
-    {
-        const uint16_t *q = (const uint16_t *)a.q + (start + tok) * a.q_stride + (g * a.G + row - tok * a.G) * HD + 8 * h;
-#pragma unroll
-        for (int k = 0; k < NK; ++k) {
-            u32x4 w = {0u, 0u, 0u, 0u};
-            if (ok) w = *(const u32x4 *)(q + 16 * k);
-            qf[k] = __builtin_bit_cast(bf16x8, w);
-        }
+    int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const PagedTilesPart part = paged_tiles_part<kTileRows, kTileKeys>(a, sh);
+    if (part.from >= part.to) {
+        if (tid == 0 && a.parts.desc) a.parts.desc[(size_t)part.w * 8 + 1] = 0;      // no unit of its own to be merged
+        return;
     }
-    f32x16 o[NDB];
-#pragma unroll
-    for (int i = 0; i < NDB; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
-    float m_run = kNoScore, l_run = 0.f;
+    const float sl2e = a.scale * 1.4426950408889634f;
+    int n_listed = 0;
+    auto field = [&](int i, int at) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(((const int *)&sh.item[wave][i])[at]); };
+#define PD_ITEM(i, f) field(i, offsetof(PagedTilesItem, f) / 4)
 
-    const int32_t *pages = p.table + (size_t)b * p.width;
-    const int t_lo = c0 / kTileKeys, t_hi = (c1 + kTileKeys - 1) / kTileKeys;
+    // the lane, for addresses that are formed where they are used: registers for them are not to be had
+    auto lane_now = [&]() __attribute__((always_inline)) {
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        return l;
+    };
+    // what is used at the ends of units alone is read there: scalar registers are short as well
+    auto rare = [&]() __attribute__((always_inline)) {
+        const PagedAttnArgs __attribute__((address_space(4))) *args = (const PagedAttnArgs __attribute__((address_space(4))) *)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(args));
+        return args;
+    };
+
+    // ---- the wave's rows of a unit ----
+    const int w0 = wave * 32;
+    int item, j, t_hi, w_min, limit;                 // of the products: listed unit, its tile, the end of them; the wave's first row sees keys
+    bf16x8 qf[NK];                                   // 0 .. w_min - 1, the lane's row 0 .. limit - 1
+    f32x16 o[NDB];
+    float m_run, l_run;
+    // four rows of the wave in the layout of whole cache lines: 8 i + lane % 8 for x[4 k + {0, 2, 1, 3}[i]]
+    auto row_of = [&](int i) __attribute__((always_inline)) { return w0 + 8 * (i >> 1 | (i & 1) << 1) + (lane_now() & 7); };
+    auto load_q = [&](int i) __attribute__((always_inline)) {
+        const auto args = rare();
+        const int G = args->G, r0 = PD_ITEM(i, r0), rows = PD_ITEM(i, rows), head = PD_ITEM(i, g) * G, start = PD_ITEM(i, start);
+        const uint16_t *q = (const uint16_t *)args->q + 8 * rows_piece(lane_now());
+        const int64_t stride = args->q_stride;
+        u32x4 x[NK];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = r0 + row_of(i), tok = row / G;
+            const uint16_t *at = q + (start + tok) * stride + (head + row - tok * G) * HD;
+#pragma unroll
+            for (int k = 0; k < NK / 4; ++k) {
+                x[4 * k + i] = u32x4{0u, 0u, 0u, 0u};
+                if (row < rows) x[4 * k + i] = *(const u32x4 *)(at + 64 * k);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < NK; ++k) qf[k] = __builtin_bit_cast(bf16x8, x[k]);
+    };
+    auto turn_q = [&]() __attribute__((always_inline)) {
+        u32x4 x[NK];
+#pragma unroll
+        for (int k = 0; k < NK; ++k) x[k] = __builtin_bit_cast(u32x4, qf[k]);
+        rows_swap8(x);
+        rows_swap16(x);
+#pragma unroll
+        for (int k = 0; k < NK; ++k) qf[k] = __builtin_bit_cast(bf16x8, x[k]);
+    };
+    auto begin = [&](int i) __attribute__((always_inline)) {
+        item = i;
+        j = PD_ITEM(i, t_lo);
+        t_hi = PD_ITEM(i, t_hi);
+        const int before = PD_ITEM(i, before), row = PD_ITEM(i, r0) + w0 + n, G = rare()->G;
+        limit = row < PD_ITEM(i, rows) ? before + row / G + 1 : 0;
+        w_min = before + (PD_ITEM(i, r0) + w0) / G + 1;
+        m_run = kNoScore;
+        l_run = 0.f;
+#pragma unroll
+        for (int i = 0; i < NDB; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+    };
 
     // ---- tile loaders ----
     // bf16: instruction i of a wave brings rows RPI (8 i + wave) .. of the tile, as a buffer that ends behind the last of them that
     // somebody sees: the lanes behind it, and all lanes where the page is not there, write zeros.  A page number is asked
-    // for one tile before its rows are.
-    const unsigned page_bytes = (unsigned)p.Hkv << p.ps_log << (HD == 128 ? 8 : 7);
-    const size_t head_bytes = ((size_t)g << p.ps_log) * (HD * 2);
-    const char *k_head = (const char *)p.k + head_bytes, *v_head = (const char *)p.v + head_bytes;
+    // for one tile before its rows are.  Page numbers and rows run ahead of the products, over the ends of units, each at a
+    // place of its own.
+    const void *k_pages = p.k, *v_pages = p.v;
+    const float *k_scales = p.k_scales, *v_scales = p.v_scales;
+    int n_pages = p.n_pages, ps_log = p.ps_log, Hkv = p.Hkv;
+    unsigned page_bytes = (unsigned)Hkv << ps_log << (HD == 128 ? 8 : 7);
+    struct Place { int item, j, t_hi; } pg, at;      // next page numbers, next rows
+    const int32_t *pages;
+    int last_key, seen;                              // of pg's unit: positions - 1; of at's: keys that it sees, kv head
+    unsigned head;
+    auto page_of = [&](int i) __attribute__((always_inline)) {
+        pg = Place{i, PD_ITEM(i, t_lo), PD_ITEM(i, t_hi)};
+        last_key = PD_ITEM(i, len) - 1;
+        // (without positions: any number will do, no key is seen)
+        const auto r = rare();
+        pages = last_key < 0 ? r->p.lens : r->p.table + (size_t)PD_ITEM(i, seq) * r->p.width;
+        last_key = max(last_key, 0);
+    };
+    auto rows_of = [&](int i) __attribute__((always_inline)) {
+        at = Place{i, PD_ITEM(i, t_lo), PD_ITEM(i, t_hi)};
+        seen = PD_ITEM(i, seen);
+        head = PD_ITEM(i, g);
+    };
+    // onto the next unit, where the place is behind its own; at the end of the list it goes on, over keys that nobody sees
+    auto settle = [&](Place &x, auto next) __attribute__((always_inline)) {
+        if (x.j < x.t_hi) return;
+        if (x.item + 1 < n_listed) next(x.item + 1);
+        else x.t_hi = 0x7fffffff;
+    };
+    auto settle_all = [&]() __attribute__((always_inline)) {
+        settle(at, rows_of);
+        settle(pg, page_of);
+    };
     unsigned k_lane, v_lane;                         // the same for every i: rows 8 RPI apart have the same swizzle
     {
         const int r = RPI * wave, lr = lane / (64 / RPI), slot = lane & (64 / RPI - 1);
@@ -124,42 +207,44 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
         v_lane = v_off<HD>(r + lr, slot) - r * HD * 2;
     }
     int ids[LPW];
-    auto ask = [&](int j) __attribute__((always_inline)) {
+    auto ask = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < LPW; ++i) ids[i] = load_const(pages, (unsigned)min(j * kTileKeys + RPI * (8 * i + wave), len - 1) >> p.ps_log);
+        for (int i = 0; i < LPW; ++i) ids[i] = load_const(pages, (unsigned)min(pg.j * kTileKeys + RPI * (8 * i + wave), last_key) >> ps_log);
+        ++pg.j;
     };
-    auto issue = [&](int j, unsigned char *st) __attribute__((always_inline)) {
+    auto issue = [&](unsigned char *st) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < LPW; ++i) {
-            const int r = RPI * (8 * i + wave), key = j * kTileKeys + r;
-            const bool there = (unsigned)ids[i] < (unsigned)p.n_pages;
-            const size_t off = (size_t)(there ? (unsigned)ids[i] : 0u) * page_bytes + (unsigned)((key & ps_mask) * (HD * 2));
-            const int bytes = __builtin_amdgcn_readfirstlane(there ? max(min(c1 - key, RPI), 0) * (HD * 2) : 0);
-            auto kb = __builtin_amdgcn_make_buffer_rsrc((void *)(k_head + off), 0, bytes, 0x00020000);
-            auto vb = __builtin_amdgcn_make_buffer_rsrc((void *)(v_head + off), 0, bytes, 0x00020000);
+            const int r = RPI * (8 * i + wave), key = at.j * kTileKeys + r;
+            const bool there = (unsigned)ids[i] < (unsigned)n_pages;
+            const size_t off = (size_t)(there ? (unsigned)ids[i] : 0u) * page_bytes + ((head << ps_log) + (unsigned)(key & ((1 << ps_log) - 1))) * (HD * 2);
+            const int bytes = __builtin_amdgcn_readfirstlane(there ? max(min(seen - key, RPI), 0) * (HD * 2) : 0);
+            auto kb = __builtin_amdgcn_make_buffer_rsrc((void *)((const char *)k_pages + off), 0, bytes, 0x00020000);
+            auto vb = __builtin_amdgcn_make_buffer_rsrc((void *)((const char *)v_pages + off), 0, bytes, 0x00020000);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(kb, (lptr_t)(st + r * HD * 2), 16, k_lane, 0, 0, 0);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(vb, (lptr_t)(st + VRING + r * HD * 2), 16, v_lane, 0, 0, 0);
         }
+        ++at.j;
     };
     // E4M3: a wave brings rows 8 wave .. + 7, eight threads a row, HD / 8 codes each; the same buffers, into registers
     constexpr int CW = HD / 32;                      // registers of codes
     unsigned kc[CW], vc[CW];
     float k_sc = 1.f, v_sc = 1.f;
-    const int cr = tid >> 3, cp = tid & 7;
-    auto ask_codes = [&](int j) __attribute__((always_inline)) {
-        ids[0] = load_const(pages, (unsigned)min(j * kTileKeys + 8 * wave, len - 1) >> p.ps_log);
+    auto ask_codes = [&]() __attribute__((always_inline)) {
+        ids[0] = load_const(pages, (unsigned)min(pg.j * kTileKeys + 8 * wave, last_key) >> ps_log);
+        ++pg.j;
     };
-    auto fetch = [&](int j) __attribute__((always_inline)) {     // the rows of tile j, whose page was asked for
-        const int key = j * kTileKeys + 8 * wave;
-        const bool there = (unsigned)ids[0] < (unsigned)p.n_pages;
+    auto fetch = [&]() __attribute__((always_inline)) {     // the rows of the tile whose page was asked for
+        const int key = at.j * kTileKeys + 8 * wave;
+        const bool there = (unsigned)ids[0] < (unsigned)n_pages;
         const unsigned id = there ? (unsigned)ids[0] : 0u;
-        const size_t off = (size_t)id * (page_bytes / 2) + (unsigned)((key & ps_mask) * HD);
-        const int bytes = __builtin_amdgcn_readfirstlane(there ? max(min(c1 - key, 8), 0) * HD : 0);
-        k_sc = load_const(p.k_scales, (size_t)id * p.Hkv + g);
-        v_sc = load_const(p.v_scales, (size_t)id * p.Hkv + g);
-        auto kb = __builtin_amdgcn_make_buffer_rsrc((void *)((const char *)p.k + head_bytes / 2 + off), 0, bytes, 0x00020000);
-        auto vb = __builtin_amdgcn_make_buffer_rsrc((void *)((const char *)p.v + head_bytes / 2 + off), 0, bytes, 0x00020000);
-        const int at_lane = (cr & 7) * HD + cp * (HD / 8);
+        const size_t off = (size_t)id * (page_bytes / 2) + ((head << ps_log) + (unsigned)(key & ((1 << ps_log) - 1))) * HD;
+        const int bytes = __builtin_amdgcn_readfirstlane(there ? max(min(seen - key, 8), 0) * HD : 0);
+        k_sc = load_const(k_scales, (size_t)id * Hkv + head);
+        v_sc = load_const(v_scales, (size_t)id * Hkv + head);
+        auto kb = __builtin_amdgcn_make_buffer_rsrc((void *)((const char *)k_pages + off), 0, bytes, 0x00020000);
+        auto vb = __builtin_amdgcn_make_buffer_rsrc((void *)((const char *)v_pages + off), 0, bytes, 0x00020000);
+        const int at_lane = lane_now() * (HD / 8);
         if constexpr (HD == 128) {
             const u32x4 kw = __builtin_amdgcn_raw_buffer_load_b128(kb, at_lane, 0, 0), vw = __builtin_amdgcn_raw_buffer_load_b128(vb, at_lane, 0, 0);
 #pragma unroll
@@ -169,6 +254,7 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
 #pragma unroll
             for (int i = 0; i < CW; ++i) { kc[i] = kw[i]; vc[i] = vw[i]; }
         }
+        ++at.j;
     };
     auto widen4 = [](unsigned lo, unsigned hi, float s) {
         return u32x4{__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false)),
@@ -177,10 +263,11 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
                      __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true))};
     };
     auto commit = [&](unsigned char *st) __attribute__((always_inline)) {
+        const int l = lane_now(), r = 8 * wave + (l >> 3);
 #pragma unroll
         for (int i = 0; i < CW / 2; ++i) {
-            *(u32x4 *)(st + k_off<HD>(cr, cp * (CW / 2) + i)) = widen4(kc[2 * i], kc[2 * i + 1], k_sc);
-            *(u32x4 *)(st + VRING + v_off<HD>(cr, cp * (CW / 2) + i)) = widen4(vc[2 * i], vc[2 * i + 1], v_sc);
+            *(u32x4 *)(st + k_off<HD>(r, (l & 7) * (CW / 2) + i)) = widen4(kc[2 * i], kc[2 * i + 1], k_sc);
+            *(u32x4 *)(st + VRING + v_off<HD>(r, (l & 7) * (CW / 2) + i)) = widen4(vc[2 * i], vc[2 * i + 1], v_sc);
         }
     };
 
@@ -195,26 +282,28 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
     bf16x8 pf[4];
     u32x4 vf[NDB][4];
     const bool late = wave >= 4;
-    auto phase_end = [&](auto M) __attribute__((always_inline)) {
+    auto phase_end = [&](auto M, bool wait = true) __attribute__((always_inline)) {
         if (KIND != PAGED_BF16) {
             if (decltype(M)::value) PD_TILE_LGKM0();     // codes written in S(j) are needed after the wave's M(j + 1)
         } else if (!decltype(M)::value) {
             PD_TILE_VMCNT(2 * LPW);
-        } else if (late) {
+        } else if (late && wait) {
             PD_TILE_VMCNT(0);
         }
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto ahead = [&](int j, auto stage) __attribute__((always_inline)) {      // in S(j); stage(i): the LDS of tile i
+    int ring;                                        // offset of the stage of the products' tile
+    auto stage = [&](int i) __attribute__((always_inline)) { return smem + ((ring + i * TILE) & (NST * TILE - 1)); };
+    auto ahead = [&]() __attribute__((always_inline)) {      // in S(j)
         if (KIND == PAGED_BF16) {
-            issue(min(j + 2, t_hi - 1), stage(j + 2));
-            ask(min(j + 3, t_hi - 1));
+            issue(stage(2));
+            ask();
         } else {
-            commit(stage(j + 2));
-            fetch(min(j + 3, t_hi - 1));
-            ask_codes(min(j + 4, t_hi - 1));
+            commit(stage(2));
+            fetch();
+            ask_codes();
         }
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -257,13 +346,16 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
     auto softmax = [&](int j, const unsigned char *st) __attribute__((always_inline)) {
         const int k0 = j * kTileKeys;
         if (k0 + kTileKeys > w_min) {                // some row of the wave does not see all of the tile
-            int seen = limit - k0 - 4 * h;
-            asm volatile("" : "+v"(seen));           // keeps the branch
+            // (by the sign of a difference: 32 conditions at once would take the scalar registers of the whole loop)
+            const int seen = limit - k0 - 4 * (lane_now() >> 5);
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (32 * kb + 8 * (r >> 2) + (r & 3) >= seen) s[kb][r] = -INFINITY;
+                for (int r = 0; r < 16; ++r) {
+                    int out = (seen - 1 - (32 * kb + 8 * (r >> 2) + (r & 3))) >> 31;
+                    asm volatile("" : "+v"(out));
+                    s[kb][r] = __builtin_bit_cast(float, (out & (int)0xff800000) | (~out & __builtin_bit_cast(int, (float)s[kb][r])));
+                }
         }
         float mx = -INFINITY;
 #pragma unroll
@@ -346,122 +438,203 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
             }
         PD_TILE_LGKM0();
     };
-    while (t_lo < t_hi) {
-        asm volatile("" : "+v"(n), "+v"(h));         // addresses are formed here, not kept from before a loop that rarely runs twice
-        auto stage_at = [&](int j) __attribute__((always_inline)) { return smem + (j - t_lo) % NST * TILE; };
-        if (KIND == PAGED_BF16) {
-            ask(t_lo);
-            issue(t_lo, smem);
-            ask(min(t_lo + 1, t_hi - 1));
-            issue(min(t_lo + 1, t_hi - 1), smem + TILE);
-            ask(min(t_lo + 2, t_hi - 1));
-        } else {
+    // ---- a unit ends: a lane holds one row's channels 32 db + 8 (r / 4) + 4 h + r % 4 ----
+    auto finish = [&]() __attribute__((always_inline)) {
+        const int r0 = PD_ITEM(item, r0), g = PD_ITEM(item, g), start = PD_ITEM(item, start), slot = PD_ITEM(item, slot);
+        const auto args = rare();
+        const int G = args->G, row = r0 + w0 + n;
+        const int rows = PD_ITEM(item, rows);
+        const bool ok = row < rows;
+        if (!clean) {
+            float zero = 0.f;                        // (infinity or NaN) * 0 is NaN, and no sum removes it
 #pragma unroll
-            for (int i = 0; i < 3; ++i) {
-                ask_codes(min(t_lo + i, t_hi - 1));
-                fetch(min(t_lo + i, t_hi - 1));
-                if (i < 2) commit(smem + i * TILE);
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) zero = fmaf(o[db][r], 0.f, zero);
+            if (__any(ok && zero != 0.f) && lane == 0) atomicOr(&bad, 1u << item);
+        } else {
+            const int32_t *table = args->p.table + (size_t)PD_ITEM(item, seq) * args->p.width;
+            const int end = min(t_hi * kTileKeys, PD_ITEM(item, seen));
+#pragma unroll 1
+            for (int key = PD_ITEM(item, t_lo) * kTileKeys; key < end; ++key) {
+                const int id = load_const(table, key >> args->p.ps_log);
+                if (id < 0 || id >= args->p.n_pages) continue;
+                const size_t unit = (size_t)id * args->p.Hkv + g, at_v = ((unit << args->p.ps_log) + (key & ((1 << args->p.ps_log) - 1))) * HD;
+                const float v_scale = KIND == PAGED_E4M3 ? load_const(args->p.v_scales, unit) : 1.f;
+#pragma unroll
+                for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const size_t i = at_v + 32 * db + 8 * (r >> 2) + 4 * h + (r & 3);
+                        const float x = KIND == PAGED_E4M3 ? e4m3_decode(((const uint8_t *)args->p.v)[i]) * v_scale : bfbits2f(((const uint16_t *)args->p.v)[i]);
+                        if (!(fabsf(x) < INFINITY) && key < limit) o[db][r] += x;
+                    }
             }
-            ask_codes(min(t_lo + 3, t_hi - 1));
         }
-        __builtin_amdgcn_sched_barrier(0);
-        if (tid == 0) again = 0;
-        if (KIND == PAGED_BF16) PD_TILE_VMCNT(2 * LPW);
-        PD_TILE_LGKM0();
-        __builtin_amdgcn_s_barrier();
-        if (late) phase_end(std::false_type{});
-        // M(t_lo)
-        if (clean) clean_v(smem);
-        load_k(smem, 0);
-        load_k(smem, 1);
+        const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
+        if (slot < 0) {
+            // halves of the wave trade registers, so that a lane has eight consecutive channels
+            const float inv = limit <= 0 ? 0.f : 1.f / l_tot;
+            u32x4 x[2 * NDB];
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int q4 = 0; q4 < 4; q4 += 2) {
+                    unsigned w[2][2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) w[i][e] = pack2bf(o[db][4 * (q4 + i) + 2 * e] * inv, o[db][4 * (q4 + i) + 2 * e + 1] * inv);
+                    const auto lo = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false), hi = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+                    x[2 * db + q4 / 2] = u32x4{lo[0], hi[0], lo[1], hi[1]};
+                }
+            rows_swap16(x);
+            rows_swap8(x);
+            uint16_t *op = (uint16_t *)args->out + 8 * rows_piece(lane_now());
+            const int Hq = args->Hq;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = r0 + row_of(i), tok = row / G;
+                uint16_t *at = op + ((size_t)(start + tok) * Hq + g * G + row - tok * G) * HD;
+#pragma unroll
+                for (int k = 0; k < NDB / 2; ++k)
+                    if (row < rows) *(u32x4 *)(at + 64 * k) = x[4 * k + i];
+            }
+        } else {
+            const size_t to = (size_t)slot * kTileRows;
+            if (h == 0 && ok) *(float2 *)(args->parts.ml + (to + w0 + n) * 2) = make_float2(m_run, l_tot);
+            float *op = args->parts.o + to * HD + 4 * rows_piece(lane_now());
+#pragma unroll
+            for (int db = 0; db < NDB; db += NDB / 2) {
+                u32x4 x[2 * NDB];
+#pragma unroll
+                for (int i = 0; i < 2 * NDB; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[i][e] = __builtin_bit_cast(unsigned, (float)o[db + i / 4][4 * (i & 3) + e]);
+                rows_swap16(x);
+                rows_swap8(x);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int row = row_of(i);
+#pragma unroll
+                    for (int k = 0; k < NDB / 2; ++k)
+                        if (r0 + row < rows) *(u32x4 *)(op + row * HD + 32 * (db + k)) = x[4 * k + i];
+                }
+            }
+        }
+    };
+    auto first_scores = [&]() __attribute__((always_inline)) {       // M's second product alone
+        if (clean) clean_v(stage(0));
+        load_k(stage(0), 0);
+        load_k(stage(0), 1);
         clear_s();
         mul_k(0);
         mul_k(1);
         __builtin_amdgcn_sched_barrier(0);
-        phase_end(std::true_type{});
-        // S(j), M(j + 1); the stages are constants, so that LDS addresses are registers plus immediates
-        int j = t_lo;
-        auto step = [&](auto STG) __attribute__((always_inline)) {
-            auto stage = [&](int i) __attribute__((always_inline)) { return smem + (decltype(STG)::value + i - j) % NST * TILE; };
-            ahead(j, stage);
-            softmax(j, stage(j));
-            phase_end(std::false_type{});
-            if (clean) clean_v(stage(j + 1));
-            products(stage(j), stage(j + 1), std::true_type{});
-            phase_end(std::true_type{});
-            return ++j < t_hi - 1;
+    };
+    // The scalar registers' values are spilled and brought back all over a range that they live through: theirs end before and
+    // behind the loop over a unit's tiles, inside of which then nothing is spilled.
+    auto anew = [](auto &...x) __attribute__((always_inline)) {
+        auto one = [](auto &v) __attribute__((always_inline)) {
+            if constexpr (sizeof(v) == 4) v = __builtin_bit_cast(std::remove_reference_t<decltype(v)>, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
+            asm volatile("" : "+s"(v));
         };
-        if (j < t_hi - 1)
-            while (step(std::integral_constant<int, 0>{}) && step(std::integral_constant<int, 1>{}) && step(std::integral_constant<int, 2>{}) &&
-                   step(std::integral_constant<int, 3>{})) {
+        (one(x), ...);
+    };
+    auto renew = [&]() __attribute__((always_inline)) {
+        anew(k_pages, v_pages, n_pages, ps_log, page_bytes, wave, ring, j, t_hi);
+        anew(at.item, at.j, at.t_hi, pg.item, pg.j, pg.t_hi, pages, last_key, seen, head, n_listed);
+#pragma unroll
+        for (int i = 0; i < (KIND == PAGED_BF16 ? LPW : 1); ++i) anew(ids[i]);
+        if (KIND != PAGED_BF16) anew(k_scales, v_scales, Hkv, k_sc, v_sc);
+    };
+    for (int first = part.from; first < part.to;) {
+        if (!clean) {
+            paged_tiles_list<kTileRows, kTileKeys>(a, sh, part, first);
+            n_listed = min(part.to - first, kListed);
+        }
+        asm volatile("" : "+v"(n), "+v"(h));         // addresses are formed here, not kept from before a loop that rarely runs twice
+        load_q(0);
+        page_of(0);
+        rows_of(0);
+        ring = 0;
+        if (KIND == PAGED_BF16) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                ask();
+                issue(smem + i * TILE);
+                settle_all();
             }
-        softmax(j, stage_at(j));
-        if (!late) phase_end(std::false_type{});
-        products(stage_at(j), nullptr, std::false_type{});
-        // (infinity or NaN) * 0 is NaN, and no sum removes it
-        float zero = 0.f;
+            ask();
+        } else {
 #pragma unroll
-        for (int db = 0; db < NDB; ++db)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) zero = fmaf(o[db][r], 0.f, zero);
-        if (__any(ok && zero != 0.f) && lane == 0) again = 1;
-        // the repeated requests of the last tile: none may land in another round's tiles or outlive the workgroup's LDS
+            for (int i = 0; i < 3; ++i) {
+                ask_codes();
+                fetch();
+                if (i < 2) commit(smem + i * TILE);
+                settle_all();
+            }
+            ask_codes();
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        begin(0);
+        turn_q();
+        if (tid == 0) bad = 0;
+        if (KIND == PAGED_BF16) PD_TILE_VMCNT(2 * LPW);
+        PD_TILE_LGKM0();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (late) phase_end(std::false_type{});
+        first_scores();                              // M of the first tile
+        phase_end(std::true_type{});
+        while (true) {
+            settle_all();
+            renew();
+            for (int left = min(t_hi - 1 - j, min(at.t_hi - at.j, pg.t_hi - pg.j)); left > 0; --left) {       // S(j), M(j + 1)
+                ahead();
+                softmax(j, stage(0));
+                phase_end(std::false_type{});
+                if (clean) clean_v(stage(1));
+                products(stage(0), stage(1), std::true_type{});
+                phase_end(std::true_type{});
+                ring = (ring + TILE) & (NST * TILE - 1);
+                ++j;
+            }
+            renew();
+            if (j < t_hi - 1) continue;
+            settle_all();
+            // the unit's last tile: between its two products the next unit's rows take the place of these
+            const bool more = item + 1 < n_listed;
+            if (more) {
+                load_q(item + 1);
+                ahead();
+            }
+            softmax(j, stage(0));
+            if (more || !late) phase_end(std::false_type{});
+            products(stage(0), nullptr, std::false_type{});
+            if (KIND == PAGED_BF16 && late && more) PD_TILE_VMCNT(0);      // here, not for the stores
+            finish();
+            if (!more) break;
+            begin(item + 1);
+            turn_q();
+            ring = (ring + TILE) & (NST * TILE - 1);
+            first_scores();
+            phase_end(std::true_type{}, false);
+        }
+        // requests behind the last tile: none may land in another round's tiles or outlive the workgroup's LDS
         if (KIND == PAGED_BF16) PD_TILE_VMCNT(0);
         __syncthreads();
-        if (clean || !again) break;
-        __syncthreads();
-        clean = true;
-        m_run = kNoScore;
-        l_run = 0.f;
-#pragma unroll
-        for (int i = 0; i < NDB; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
-    }
-    if (clean)
-#pragma unroll 1
-        for (int key = c0; key < c1; ++key) {
-            const int id = load_const(pages, key >> p.ps_log);
-            if (id < 0 || id >= p.n_pages) continue;
-            const size_t unit = (size_t)id * p.Hkv + g, at_v = ((unit << p.ps_log) + (key & ps_mask)) * HD;
-            const float v_scale = KIND == PAGED_E4M3 ? load_const(p.v_scales, unit) : 1.f;
-#pragma unroll
-            for (int db = 0; db < NDB; ++db)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const size_t i = at_v + 32 * db + 8 * (r >> 2) + 4 * h + (r & 3);
-                    const float x = KIND == PAGED_E4M3 ? e4m3_decode(((const uint8_t *)p.v)[i]) * v_scale : bfbits2f(((const uint16_t *)p.v)[i]);
-                    if (!(fabsf(x) < INFINITY) && key < limit) o[db][r] += x;
-                }
+        const unsigned redo = clean ? 0u : __builtin_amdgcn_readfirstlane(bad);
+        clean = redo != 0;
+        if (clean) {
+            if (lane == 0)
+                for (int i = 0, to = 0; i < n_listed; ++i)
+                    if (redo >> i & 1) sh.item[wave][to++] = sh.item[wave][i];
+            n_listed = __popc(redo);
+            __syncthreads();                         // bad is read
+        } else {
+            first += kListed;
         }
-
-    // ---- a lane holds row `row`, channels 32 db + 8 (r / 4) + 4 h + r % 4 ----
-    const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
-    if (nc_u == 1) {
-        // halves of the wave trade registers, so that a lane stores eight consecutive channels
-        const float inv = limit <= 0 ? 0.f : 1.f / l_tot;
-        uint16_t *op = (uint16_t *)a.out + ((size_t)(start + tok) * a.Hq + g * a.G + row - tok * a.G) * HD + 8 * h;
-#pragma unroll
-        for (int db = 0; db < NDB; ++db)
-#pragma unroll
-            for (int q4 = 0; q4 < 4; q4 += 2) {
-                unsigned w[2][2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) w[i][e] = pack2bf(o[db][4 * (q4 + i) + 2 * e] * inv, o[db][4 * (q4 + i) + 2 * e + 1] * inv);
-                const auto lo = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false), hi = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
-                if (ok) *(u32x4 *)(op + 32 * db + 8 * q4) = u32x4{lo[0], hi[0], lo[1], hi[1]};
-            }
-    } else if (ok) {
-        const size_t at_part = (size_t)(part0 + c) * kTileRows + w0 + n;
-        float *op = a.parts.o + at_part * HD + 4 * h;
-#pragma unroll
-        for (int db = 0; db < NDB; ++db)
-#pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4)
-                *(float4 *)(op + 32 * db + 8 * q4) = make_float4(o[db][4 * q4], o[db][4 * q4 + 1], o[db][4 * q4 + 2], o[db][4 * q4 + 3]);
-        if (h == 0) *(float2 *)(a.parts.ml + at_part * 2) = make_float2(m_run, l_tot);
     }
 }
 

@@ -1,11 +1,10 @@
-// The division of a paged attention call's keys into work items, on the device (shared by its two kernels).
+// The division of a paged attention call's keys over its workgroups, on the device (shared by its two kernels).
 //
-// A unit is a tile of R (token, head) rows of one sequence and kv head; an item is one of the chunks that a unit's keys are
-// divided into.  Lengths are known on the device alone, so every workgroup works the division out for itself: the keys that
-// all units have to read, divided by the items aimed for, is the chunk; a sequence of len keys and U units makes
-// U ceil(len / chunk) items, and since U (len / chunk + 1) <= 2 U len / chunk where there is more than one chunk, the split
-// ones are at most twice the items aimed for.  A thread keeps the counts of its own consecutive sequences and the
-// sum of those before; nothing is stored per sequence.
+// A unit is a tile of R (token, head) rows of one sequence and kv head.  All units' keys, unit after unit, form one stream, and
+// workgroup w takes the w-th of equal parts of it, whatever units they belong to.  All workgroups then have the same work, a unit
+// is split only where a border falls into it, and a workgroup has at most two partials: of the unit that it ends (slot 2 w) and
+// of the one that it begins (slot 2 w + 1).  Lengths are known on the device alone, so every workgroup works the division out for
+// itself.  A thread keeps the sums of its own consecutive sequences and of those before; nothing is stored per sequence.
 #pragma once
 #include <type_traits>
 
@@ -15,26 +14,15 @@ namespace pd {
 
 __device__ __forceinline__ float pexp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-struct PagedItems {
-    int chunk, total, split_units;       // keys of a chunk; items and split units of the call, per kv head
-    int b0, b1;                          // this thread's sequences
-    int first, own;                      // items ahead of them, and theirs
-    int split, unit;                     // split items and split units ahead of them
-    int start, rows, len;                // the first of them
-};
-struct PagedFound {
-    int seq, at;                         // sequence of an item, and the item's place among the sequence's
-    int units, chunks, start, rows, len; // of the sequence
-    int split, unit;                     // split items and split units ahead of the sequence
-};
-
 // Sum over the lanes up to this one, by data-parallel moves: a cross-lane step through LDS would take ten times as long, and every
 // workgroup waits for the division before its first load.
 template <typename T>
 __device__ __forceinline__ T wave_scan(T v)
 {
     auto add = [&](auto CTRL, auto ROWS) {
-        const int m = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(CTRL)::value, decltype(ROWS)::value, 0xf, true);
+        struct W { int w[sizeof(T) / 4]; } m = __builtin_bit_cast(W, v);
+#pragma unroll
+        for (int &w : m.w) w = __builtin_amdgcn_update_dpp(0, w, decltype(CTRL)::value, decltype(ROWS)::value, 0xf, true);
         v += __builtin_bit_cast(T, m);
     };
     add(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});    // one lane up, inside rows of 16
@@ -53,9 +41,27 @@ __device__ __forceinline__ int paged_units(const PagedAttnArgs &a, int n)
     return rows > a.rows_above && rows <= a.rows_most ? (rows + R - 1) / R : 0;
 }
 __device__ __forceinline__ int paged_chunks(int len, int chunk) { return max((len + chunk - 1) / chunk, 1); }
+// a thread's sequences, and the first of them
+struct PagedOwn {
+    int b0, b1, start, rows, len;
+};
+template <int NT>
+__device__ __forceinline__ PagedOwn paged_own(const PagedAttnArgs &a)
+{
+    const int n = a.p.n_seqs, per = (n + NT - 1) / NT;
+    PagedOwn r = {};
+    r.b0 = min((int)threadIdx.x * per, n);
+    r.b1 = min(r.b0 + per, n);
+    if (r.b0 < n) {
+        r.start = paged_start(a.p, r.b0);
+        r.rows = paged_rows(a.p, r.b0, r.start);
+        r.len = paged_len(a.p, r.b0);
+    }
+    return r;
+}
 // f(sequence, first row, rows, positions) for a thread's sequences; the first one's fields are kept, most calls have no more
 template <typename F>
-__device__ __forceinline__ void paged_each(const PagedAttnArgs &a, const PagedItems &r, F f)
+__device__ __forceinline__ void paged_each(const PagedAttnArgs &a, const PagedOwn &r, F f)
 {
     if (r.b0 < r.b1) f(r.b0, r.start, r.rows, r.len);
     for (int b = r.b0 + 1; b < r.b1; ++b) {
@@ -63,110 +69,24 @@ __device__ __forceinline__ void paged_each(const PagedAttnArgs &a, const PagedIt
         f(b, start, paged_rows(a.p, b, start), paged_len(a.p, b));
     }
 }
-// LDS of the division
-template <int NT>
-struct PagedShared {
-    float keys[NT / 64], rows[NT / 64];
-    int own[NT / 64], split[NT / 64], unit[NT / 64];
-    PagedFound found;
-};
-// By all NT threads.  Sums that only steer the division are fp32: every workgroup forms them in the same order, and the rows'
-// is exact up to 2^24, which no call has more of.
-template <int R, int NT>
-__device__ __forceinline__ PagedItems paged_divide(const PagedAttnArgs &a, PagedShared<NT> &sh)
+
+__device__ __forceinline__ void paged_describe(const PagedAttnArgs &a, int unit, int part0, int parts, int start, int r0, int rows, int g,
+                                               int before)
 {
-    const int n = a.p.n_seqs, per = (n + NT - 1) / NT, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    PagedItems r = {64, 0, 0, min((int)threadIdx.x * per, n), 0, 0, 0, 0, 0, 0, 0, 0};
-    r.b1 = min(r.b0 + per, n);
-    if (r.b0 < n) {
-        r.start = paged_start(a.p, r.b0);
-        r.rows = paged_rows(a.p, r.b0, r.start);
-        r.len = paged_len(a.p, r.b0);
-    }
-    float keys = 0.f, rows = 0.f;
-    paged_each(a, r, [&](int, int, int n_rows, int len) {
-        keys += (float)paged_units<R>(a, n_rows) * (float)len;
-        rows += (float)n_rows;
-    });
-    keys = wave_scan(keys);
-    rows = wave_scan(rows);
-    if (lane == 63) {
-        sh.keys[wave] = keys;
-        sh.rows[wave] = rows;
-    }
-    __syncthreads();
-    keys = rows = 0.f;
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) {
-        keys += sh.keys[w];
-        rows += sh.rows[w];
-    }
-    if (rows > (float)a.p.n_rows) return r;          // the sequences' rows overlap: no such call, and nothing is done
-    // (1 + 2^-10: more than the roundings of the sum, so that the bound on the split items holds)
-    const float chunk = keys * (float)a.p.Hkv * (1.0009765625f / (float)a.target);
-    r.chunk = ((int)ceilf(fminf(fmaxf(chunk, (float)a.least), (float)((1 << 30) - 128))) + 63) & ~63;
-    int own = 0, split = 0, unit = 0;
-    paged_each(a, r, [&](int, int, int n_rows, int len) {
-        const int u = paged_units<R>(a, n_rows), nc = paged_chunks(len, r.chunk);
-        own += u * nc;
-        split += nc > 1 ? u * nc : 0;
-        unit += nc > 1 ? u : 0;
-    });
-    const int own_to = wave_scan(own), split_to = wave_scan(split), unit_to = wave_scan(unit);
-    if (lane == 63) {
-        sh.own[wave] = own_to;
-        sh.split[wave] = split_to;
-        sh.unit[wave] = unit_to;
-    }
-    __syncthreads();
-    r.own = own;
-    r.first = own_to - own;
-    r.split = split_to - split;
-    r.unit = unit_to - unit;
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) {
-        if (w < wave) {
-            r.first += sh.own[w];
-            r.split += sh.split[w];
-            r.unit += sh.unit[w];
-        }
-        r.total += sh.own[w];
-        r.split_units += sh.unit[w];
-    }
-    r.total = __builtin_amdgcn_readfirstlane(r.total);
-    r.chunk = __builtin_amdgcn_readfirstlane(r.chunk);
-    return r;
-}
-// Item t < it.total, written by the thread that has it; ends with a barrier.
-template <int R>
-__device__ __forceinline__ void paged_find(const PagedAttnArgs &a, const PagedItems &it, int t, PagedFound *f)
-{
-    if (t >= it.first && t < it.first + it.own) {
-        int run = it.first, split = it.split, unit = it.unit;
-        paged_each(a, it, [&](int b, int start, int rows, int len) {
-            const int u = paged_units<R>(a, rows), nc = paged_chunks(len, it.chunk);
-            if (t >= run && t < run + u * nc) {
-                f->seq = b; f->at = t - run; f->units = u; f->chunks = nc; f->split = split; f->unit = unit;
-                f->start = start; f->rows = rows; f->len = len;
-            }
-            run += u * nc;
-            split += nc > 1 ? u * nc : 0;
-            unit += nc > 1 ? u : 0;
-        });
-    }
-    __syncthreads();
+    int32_t *d = a.parts.desc + (size_t)unit * 8;
+    d[0] = part0; d[1] = parts; d[2] = start; d[3] = r0; d[4] = rows; d[5] = g; d[6] = before;
 }
 
-// ---- the division into equal streams --------------------------------------------------------------------------------------
-//
-// For the kernel that is bound by reading keys: all units' keys in blocks of `gran`, unit after unit (sequence, kv head, row
-// tile), form one stream, and workgroup w of W takes blocks w per .. (w + 1) per - 1 of it, whatever units they belong to.  All
-// workgroups then read the same number of keys, a unit is split only where a border falls into it, and a workgroup has at
-// most two partials: of the unit that it ends (slot 2 w) and of the one that it begins (slot 2 w + 1).
+// ---- few rows: bound by reading keys; blocks of `gran` keys are counted, each unit of a sequence has as many -------------
+template <int NT>
+struct PagedShared {
+    float blocks[NT / 64], rows[NT / 64];
+    int own[NT / 64];
+};
 struct PagedStream {
     int gran, total, per;                // keys of a block; blocks of the call and of a workgroup
-    int b0, b1, first;                   // this thread's sequences, and the blocks ahead of them
-    int start, rows, len;                // the first of them
+    int first;                           // blocks ahead of this thread's sequences
+    PagedOwn own;
 };
 struct PagedPiece {
     int seq, start, rows, len;           // sequence of a block
@@ -176,15 +96,8 @@ struct PagedPiece {
 template <int R, int NT, int BASE>
 __device__ __forceinline__ PagedStream paged_stream(const PagedAttnArgs &a, PagedShared<NT> &sh)
 {
-    const int n = a.p.n_seqs, per = (n + NT - 1) / NT, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    PagedItems r = {};
-    r.b0 = min((int)threadIdx.x * per, n);
-    r.b1 = min(r.b0 + per, n);
-    if (r.b0 < n) {
-        r.start = paged_start(a.p, r.b0);
-        r.rows = paged_rows(a.p, r.b0, r.start);
-        r.len = paged_len(a.p, r.b0);
-    }
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const PagedOwn r = paged_own<NT>(a);
     float blocks = 0.f, rows = 0.f;
     paged_each(a, r, [&](int, int, int n_rows, int len) {
         blocks += (float)paged_units<R>(a, n_rows) * (float)((len + BASE - 1) / BASE);
@@ -193,17 +106,17 @@ __device__ __forceinline__ PagedStream paged_stream(const PagedAttnArgs &a, Page
     blocks = wave_scan(blocks);
     rows = wave_scan(rows);
     if (lane == 63) {
-        sh.keys[wave] = blocks;
+        sh.blocks[wave] = blocks;
         sh.rows[wave] = rows;
     }
     __syncthreads();
     blocks = rows = 0.f;
 #pragma unroll
     for (int w = 0; w < NT / 64; ++w) {
-        blocks += sh.keys[w];
+        blocks += sh.blocks[w];
         rows += sh.rows[w];
     }
-    PagedStream st = {BASE, 0, 1, r.b0, r.b1, 0, r.start, r.rows, r.len};
+    PagedStream st = {BASE, 0, 1, 0, r};
     if (rows > (float)a.p.n_rows) return st;         // the sequences' rows overlap: no such call, and nothing is done
     // larger blocks where their number would not fit an int32 (a sequence without keys is a block too, hence the margin)
     for (float x = blocks * (float)a.p.Hkv; x > (float)(1 << 29); x *= 0.5f) st.gran *= 2;
@@ -226,11 +139,9 @@ __device__ __forceinline__ PagedStream paged_stream(const PagedAttnArgs &a, Page
 template <int R>
 __device__ __forceinline__ void paged_locate(const PagedAttnArgs &a, const PagedStream &st, int t, PagedPiece *f)
 {
-    PagedItems r = {};
-    r.b0 = st.b0; r.b1 = st.b1; r.start = st.start; r.rows = st.rows; r.len = st.len;
     if (t >= st.first) {
         int run = st.first;
-        paged_each(a, r, [&](int b, int start, int rows, int len) {
+        paged_each(a, st.own, [&](int b, int start, int rows, int len) {
             const int u = paged_units<R>(a, rows), nb = paged_chunks(len, st.gran), n = a.p.Hkv * u * nb;
             if (t >= run && t < run + n) {
                 f->seq = b; f->start = start; f->rows = rows; f->len = len; f->before = run; f->blocks = nb; f->units = u;
@@ -241,11 +152,195 @@ __device__ __forceinline__ void paged_locate(const PagedAttnArgs &a, const Paged
     __syncthreads();
 }
 
-__device__ __forceinline__ void paged_describe(const PagedAttnArgs &a, int unit, int part0, int parts, int start, int r0, int rows, int g,
-                                               int before)
+// ---- many rows: bound by the matrix pipe; a unit's tiles of keys are what its last row sees ---------------------------------
+//
+// Row tile u of a sequence is counted with G (kUnitKeys + before) + R (u + 1), G times the keys that it sees and those that going from one
+// unit to the next takes the time of; inside a unit the count is proportional to its tiles.  The units of a sequence and kv head are
+// taken from both ends in turn (the last row tile, the first, the last but one, ..), which makes all pairs count the same: what is
+// ahead of a unit has a closed form, and where the parts hold whole pairs, as those of equal prompts mostly do, nothing is split.
+// A border closer than `margin` to an end of its unit moves there: a partial of few tiles costs more than the
+// unevenness.  Every workgroup finds the same cut for a border, and as tiles count less than `per` each, cuts inside a unit are
+// different tiles.
+constexpr int kUnitKeys = 256, kListed = 16;
+constexpr int kCutTiles = 8;             // a unit of fewer tiles is never split
+struct PagedTilesItem {
+    int seq, g, start, r0;               // sequence, kv head, first row of the sequence, first (token, head) row of the unit
+    int rows, before, t_lo, t_hi;        // (token, head) rows of the sequence, position of its first row, tiles
+    int seen, slot, len, pad;            // keys that the unit sees; partial, or -1; positions of the sequence
+};
+struct PagedTilesSeq {
+    long long at;                        // count and units ahead of the sequence
+    int unit, seq, start, rows, len, pad;
+};
+struct PagedCut {
+    int unit, tile;
+};
+template <int NT>
+struct PagedTilesShared {
+    long long count[NT / 64];
+    int units[NT / 64];
+    float rows[NT / 64];
+    PagedTilesSeq border[2], of[kListed];            // the sequences of the workgroup's borders and listed units
+    PagedTilesItem item[NT / 64][kListed];           // each wave's own copy
+};
+struct PagedTilesPart {
+    long long per, margin;               // count of a workgroup; see above
+    long long first;                     // count and units ahead of this thread's sequences
+    int w;                               // the workgroup's place
+    int first_units, from, to;           // units of the workgroup: from .. to - 1, the first from tile `tile`, the last up to tile_to
+    int tile, tile_to;
+    PagedOwn own;
+};
+// a / b of numbers below 2^53, by way of double: a tenth of the instructions of the compiler's 64-bit division
+__device__ __forceinline__ int paged_quotient(long long a, long long b)
 {
-    int32_t *d = a.parts.desc + (size_t)unit * 8;
-    d[0] = part0; d[1] = parts; d[2] = start; d[3] = r0; d[4] = rows; d[5] = g; d[6] = before;
+    int q = (int)((double)a / (double)b);
+    if (a - q * b < 0) --q;
+    if (a - q * b >= b) ++q;
+    return q;
+}
+template <int R, int TK>
+struct PagedUnits {                      // of a sequence and kv head
+    int units, rows, before;
+    long long each, pair, all;           // each + R (u + 1): count of row tile u; count of a pair and of all units
+    __device__ __forceinline__ PagedUnits(const PagedAttnArgs &a, int n_rows, int len)
+    {
+        units = paged_units<R>(a, n_rows);
+        rows = n_rows * a.G;
+        before = len - n_rows;
+        each = (long long)a.G * (kUnitKeys + max(before, 0));
+        pair = 2 * each + (long long)R * (units + 1);
+        all = ahead(units);
+    }
+    __device__ __forceinline__ int tile(int i) const { return i & 1 ? i >> 1 : units - 1 - (i >> 1); }      // row tile of unit i
+    __device__ __forceinline__ long long count(int u) const { return each + (long long)R * (u + 1); }
+    __device__ __forceinline__ long long ahead(int i) const { return (i >> 1) * pair + (i & 1 ? count(tile(i - 1)) : 0); }
+    __device__ __forceinline__ int seen(const PagedAttnArgs &a, int u) const { return max(before + (min(R * (u + 1), rows) - 1) / a.G + 1, 0); }
+    __device__ __forceinline__ int tiles(int seen) const { return max((seen + TK - 1) / TK, 1); }
+    // (more rows than positions: the count says too little about the tiles)
+    __device__ __forceinline__ bool whole(int tiles) const { return tiles < kCutTiles || before < 0; }
+};
+template <int R, int TK, int NT>
+__device__ __forceinline__ PagedTilesPart paged_tiles_part(const PagedAttnArgs &a, PagedTilesShared<NT> &sh)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, Hkv = a.p.Hkv;
+    PagedTilesPart r = {};
+    r.own = paged_own<NT>(a);
+    long long count = 0;
+    int units = 0;
+    float rows = 0.f;                    // exact up to 2^24, which no call has more of
+    paged_each(a, r.own, [&](int, int, int n_rows, int len) {
+        const PagedUnits<R, TK> s(a, n_rows, len);
+        count += Hkv * s.all;
+        units += Hkv * s.units;
+        rows += (float)n_rows;
+    });
+    // Neighbours in the stream read the same keys, so those of an XCD, which are every eighth workgroup, are neighbours: four
+    // prompts of 2048 tokens, 32 heads on 8, take 195 us so and 200 us in the workgroups' own order
+    const int W = gridDim.x, xcd = blockIdx.x & 7;
+    r.w = xcd * (W >> 3) + min(xcd, W & 7) + (blockIdx.x >> 3);
+    const long long count_to = wave_scan(count);
+    const int units_to = wave_scan(units);
+    rows = wave_scan(rows);
+    if (lane == 63) {
+        sh.count[wave] = count_to;
+        sh.units[wave] = units_to;
+        sh.rows[wave] = rows;
+    }
+    __syncthreads();
+    r.first = count_to - count;
+    r.first_units = units_to - units;
+    long long total = 0;
+    int total_units = 0;
+    rows = 0.f;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+        if (w < wave) {
+            r.first += sh.count[w];
+            r.first_units += sh.units[w];
+        }
+        total += sh.count[w];
+        total_units += sh.units[w];
+        rows += sh.rows[w];
+    }
+    if (rows > (float)a.p.n_rows) total = 0;         // the sequences' rows overlap: no such call, and nothing is done
+    r.per = max((long long)(paged_quotient(total, W) + 1LL), (long long)a.least * TK * a.G);
+    r.margin = max((long long)kCutTiles / 2 * TK * a.G, r.per / 32);
+    if (total == 0 || r.w * r.per >= total) return r;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const long long border = (r.w + i) * r.per;
+        if (border < r.first || border >= r.first + count) continue;
+        long long at = r.first;
+        int unit = r.first_units;
+        paged_each(a, r.own, [&](int b, int start, int n_rows, int len) {
+            const PagedUnits<R, TK> s(a, n_rows, len);
+            if (border >= at && border < at + Hkv * s.all) sh.border[i] = PagedTilesSeq{at, unit, b, start, n_rows, len, 0};
+            at += Hkv * s.all;
+            unit += Hkv * s.units;
+        });
+    }
+    __syncthreads();
+    PagedCut cut = {total_units, 0};                 // of border lane % 2
+    const long long border = (r.w + (lane & 1)) * r.per;
+    if (border < total) {
+        const PagedTilesSeq q = sh.border[lane & 1];
+        const PagedUnits<R, TK> s(a, q.rows, q.len);
+        long long y = border - q.at;
+        const int g = paged_quotient(y, s.all);
+        y -= g * s.all;
+        int i = 2 * paged_quotient(y, s.pair);
+        y -= (i >> 1) * s.pair;
+        const long long first_of_pair = s.count(s.tile(i));
+        if (i + 1 < s.units && y >= first_of_pair) {
+            ++i;
+            y -= first_of_pair;
+        }
+        const long long of = s.count(s.tile(i));
+        const int tiles = s.tiles(s.seen(a, s.tile(i)));
+        const bool inside = !s.whole(tiles) && y >= r.margin && y <= of - r.margin;
+        const bool next = !inside && 2 * y >= of;
+        cut = PagedCut{q.unit + g * s.units + i + next, inside ? min(max((int)((double)y * tiles / (double)of), 1), tiles - 1) : 0};
+    }
+    r.from = __builtin_amdgcn_readlane(cut.unit, 0);
+    r.tile = __builtin_amdgcn_readlane(cut.tile, 0);
+    r.tile_to = __builtin_amdgcn_readlane(cut.tile, 1);
+    r.to = __builtin_amdgcn_readlane(cut.unit, 1) + (r.tile_to > 0);
+    return r;
+}
+// The list of units first .. first + kListed - 1 of the workgroup; a wave writes its copy, thread 0 describes the unit that the
+// workgroup begins and does not end.  All threads come here, which is a barrier for what they read of an earlier list.
+template <int R, int TK, int NT>
+__device__ __forceinline__ void paged_tiles_list(const PagedAttnArgs &a, PagedTilesShared<NT> &sh, const PagedTilesPart &part, int first)
+{
+    const int Hkv = a.p.Hkv, end = min(first + kListed, part.to), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int unit = part.first_units;
+    long long at = part.first;
+    __syncthreads();
+    if (unit < end)
+        paged_each(a, part.own, [&](int b, int start, int n_rows, int len) {
+            const PagedUnits<R, TK> s(a, n_rows, len);
+            for (int k = max(first, unit); k < min(end, unit + Hkv * s.units); ++k) sh.of[k - first] = PagedTilesSeq{at, unit, b, start, n_rows, len, 0};
+            unit += Hkv * s.units;
+            at += Hkv * s.all;
+        });
+    __syncthreads();
+    if (first + lane < end) {
+        const PagedTilesSeq q = sh.of[lane];
+        const PagedUnits<R, TK> s(a, q.rows, q.len);
+        const int k = first + lane, g = (k - q.unit) / s.units, i = k - q.unit - g * s.units, u = s.tile(i), seen = s.seen(a, u), tiles = s.tiles(seen);
+        const int lo = k == part.from ? part.tile : 0, hi = k == part.to - 1 && part.tile_to ? part.tile_to : tiles;
+        const int slot = lo > 0 ? 2 * part.w : hi < tiles ? 2 * part.w + 1 : -1;
+        sh.item[wave][lane] = PagedTilesItem{q.seq, g, q.start, u * R, s.rows, s.before, lo, hi, seen, slot, q.len, 0};
+        if (wave == 0 && k == part.to - 1 && a.parts.desc) {
+            int parts = 0;
+            if (lo == 0 && hi < tiles) {
+                const long long u0 = q.at + g * s.all + s.ahead(i), u1 = u0 + s.count(u);
+                parts = 2 + paged_quotient(u1 - part.margin, part.per) - paged_quotient(u0 + part.margin + part.per - 1, part.per);
+            }
+            paged_describe(a, part.w, slot, parts, q.start, u * R, s.rows, g, s.before);
+        }
+    }
 }
 
 }  // namespace pd
