@@ -129,13 +129,10 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
         u32x4 x[NK];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int row = r0 + row_of(i), tok = row / G;
+            const int row = min(r0 + row_of(i), rows - 1), tok = row / G;    // (rows behind the last are not stored)
             const uint16_t *at = q + (start + tok) * stride + (head + row - tok * G) * HD;
 #pragma unroll
-            for (int k = 0; k < NK / 4; ++k) {
-                x[4 * k + i] = u32x4{0u, 0u, 0u, 0u};
-                if (row < rows) x[4 * k + i] = *(const u32x4 *)(at + 64 * k);
-            }
+            for (int k = 0; k < NK / 4; ++k) x[4 * k + i] = *(const u32x4 *)(at + 64 * k);
         }
 #pragma unroll
         for (int k = 0; k < NK; ++k) qf[k] = __builtin_bit_cast(bf16x8, x[k]);
@@ -605,10 +602,8 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
             settle_all();
             // the unit's last tile: between its two products the next unit's rows take the place of these
             const bool more = item + 1 < n_listed;
-            if (more) {
-                load_q(item + 1);
-                ahead();
-            }
+            load_q(min(item + 1, n_listed - 1));
+            ahead();
             softmax(j, stage(0));
             if (more || !late) phase_end(std::false_type{});
             products(stage(0), nullptr, std::false_type{});
