@@ -119,18 +119,31 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
     bf16x8 qf[NK];                                   // 0 .. w_min - 1, the lane's row 0 .. limit - 1
     f32x16 o[NDB];
     float m_run, l_run;
+    // A unit's row w is (token, head) row r0 + w of its sequence: token tok + (rest + w) / G, where G tok + rest = r0.  The quotient by
+    // way of fp32 is exact for dividends up to 2^21.
+    struct Unit {
+        int r0, rows, tok, rest, start, head, G;
+        float per_G;
+        __device__ __forceinline__ int token(int w) const { return (int)(((float)(rest + w) + 0.5f) * per_G); }
+    };
+    auto unit_of = [&](int i, int G) __attribute__((always_inline)) {
+        Unit u = {PD_ITEM(i, r0), PD_ITEM(i, rows), PD_ITEM(i, tok), 0, PD_ITEM(i, start), PD_ITEM(i, g) * G, G, 1.f / (float)G};
+        u.rest = u.r0 - u.tok * G;
+        return u;
+    };
     // four rows of the wave in the layout of whole cache lines: 8 i + lane % 8 for x[4 k + {0, 2, 1, 3}[i]]
     auto row_of = [&](int i) __attribute__((always_inline)) { return w0 + 8 * (i >> 1 | (i & 1) << 1) + (lane_now() & 7); };
     auto load_q = [&](int i) __attribute__((always_inline)) {
         const auto args = rare();
-        const int G = args->G, r0 = PD_ITEM(i, r0), rows = PD_ITEM(i, rows), head = PD_ITEM(i, g) * G, start = PD_ITEM(i, start);
-        const uint16_t *q = (const uint16_t *)args->q + 8 * rows_piece(lane_now());
+        const Unit u = unit_of(i, args->G);
         const int64_t stride = args->q_stride;
+        const uint16_t *q = (const uint16_t *)args->q + (u.start + u.tok) * stride + (u.head + u.rest) * HD;
+        const int piece = 8 * rows_piece(lane_now());
         u32x4 x[NK];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int row = min(r0 + row_of(i), rows - 1), tok = row / G;    // (rows behind the last are not stored)
-            const uint16_t *at = q + (start + tok) * stride + (head + row - tok * G) * HD;
+            const int w = min(row_of(i), u.rows - 1 - u.r0), tok = u.token(w);    // (rows behind the last are not stored)
+            const uint16_t *at = q + tok * stride + ((w - tok * u.G) * HD + piece);
 #pragma unroll
             for (int k = 0; k < NK / 4; ++k) x[4 * k + i] = *(const u32x4 *)(at + 64 * k);
         }
@@ -146,13 +159,19 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
 #pragma unroll
         for (int k = 0; k < NK; ++k) qf[k] = __builtin_bit_cast(bf16x8, x[k]);
     };
-    auto begin = [&](int i) __attribute__((always_inline)) {
+    // what the products need of a unit
+    struct Bounds { int t_lo, t_hi, w_min, limit; };
+    auto bounds_of = [&](int i) __attribute__((always_inline)) {
+        const Unit u = unit_of(i, rare()->G);
+        const int first = PD_ITEM(i, before) + u.tok + 1;
+        return Bounds{PD_ITEM(i, t_lo), PD_ITEM(i, t_hi), first + __builtin_amdgcn_readfirstlane(u.token(w0)), w0 + n < u.rows - u.r0 ? first + u.token(w0 + n) : 0};
+    };
+    auto begin = [&](int i, const Bounds &x) __attribute__((always_inline)) {
         item = i;
-        j = PD_ITEM(i, t_lo);
-        t_hi = PD_ITEM(i, t_hi);
-        const int before = PD_ITEM(i, before), row = PD_ITEM(i, r0) + w0 + n, G = rare()->G;
-        limit = row < PD_ITEM(i, rows) ? before + row / G + 1 : 0;
-        w_min = before + (PD_ITEM(i, r0) + w0) / G + 1;
+        j = x.t_lo;
+        t_hi = x.t_hi;
+        w_min = x.w_min;
+        limit = x.limit;
         m_run = kNoScore;
         l_run = 0.f;
 #pragma unroll
@@ -204,37 +223,34 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
         v_lane = v_off<HD>(r + lr, slot) - r * HD * 2;
     }
     int ids[LPW];
-    auto ask = [&]() __attribute__((always_inline)) {
+    auto ask = [&](int (&ids)[LPW]) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < LPW; ++i) ids[i] = load_const(pages, (unsigned)min(pg.j * kTileKeys + RPI * (8 * i + wave), last_key) >> ps_log);
         ++pg.j;
     };
-    auto issue = [&](unsigned char *st) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < LPW; ++i) {
-            const int r = RPI * (8 * i + wave), key = at.j * kTileKeys + r;
-            const bool there = (unsigned)ids[i] < (unsigned)n_pages;
-            const size_t off = (size_t)(there ? (unsigned)ids[i] : 0u) * page_bytes + ((head << ps_log) + (unsigned)(key & ((1 << ps_log) - 1))) * (HD * 2);
-            const int bytes = __builtin_amdgcn_readfirstlane(there ? max(min(seen - key, RPI), 0) * (HD * 2) : 0);
-            auto kb = __builtin_amdgcn_make_buffer_rsrc((void *)((const char *)k_pages + off), 0, bytes, 0x00020000);
-            auto vb = __builtin_amdgcn_make_buffer_rsrc((void *)((const char *)v_pages + off), 0, bytes, 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(kb, (lptr_t)(st + r * HD * 2), 16, k_lane, 0, 0, 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(vb, (lptr_t)(st + VRING + r * HD * 2), 16, v_lane, 0, 0, 0);
-        }
-        ++at.j;
+    auto issue = [&](unsigned char *st, int i, const int (&ids)[LPW]) __attribute__((always_inline)) {
+        const int r = RPI * (8 * i + wave), key = at.j * kTileKeys + r;
+        const bool there = (unsigned)ids[i] < (unsigned)n_pages;
+        const size_t off = (size_t)(there ? (unsigned)ids[i] : 0u) * page_bytes + ((head << ps_log) + (unsigned)(key & ((1 << ps_log) - 1))) * (HD * 2);
+        const int bytes = __builtin_amdgcn_readfirstlane(there ? max(min(seen - key, RPI), 0) * (HD * 2) : 0);
+        auto kb = __builtin_amdgcn_make_buffer_rsrc((void *)((const char *)k_pages + off), 0, bytes, 0x00020000);
+        auto vb = __builtin_amdgcn_make_buffer_rsrc((void *)((const char *)v_pages + off), 0, bytes, 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(kb, (lptr_t)(st + r * HD * 2), 16, k_lane, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(vb, (lptr_t)(st + VRING + r * HD * 2), 16, v_lane, 0, 0, 0);
+        if (i == LPW - 1) ++at.j;
     };
     // E4M3: a wave brings rows 8 wave .. + 7, eight threads a row, HD / 8 codes each; the same buffers, into registers
     constexpr int CW = HD / 32;                      // registers of codes
     unsigned kc[CW], vc[CW];
     float k_sc = 1.f, v_sc = 1.f;
-    auto ask_codes = [&]() __attribute__((always_inline)) {
-        ids[0] = load_const(pages, (unsigned)min(pg.j * kTileKeys + 8 * wave, last_key) >> ps_log);
+    auto ask_codes = [&](int &id) __attribute__((always_inline)) {
+        id = load_const(pages, (unsigned)min(pg.j * kTileKeys + 8 * wave, last_key) >> ps_log);
         ++pg.j;
     };
-    auto fetch = [&]() __attribute__((always_inline)) {     // the rows of the tile whose page was asked for
+    auto fetch = [&](int asked) __attribute__((always_inline)) {     // the rows of the tile whose page was asked for
         const int key = at.j * kTileKeys + 8 * wave;
-        const bool there = (unsigned)ids[0] < (unsigned)n_pages;
-        const unsigned id = there ? (unsigned)ids[0] : 0u;
+        const bool there = (unsigned)asked < (unsigned)n_pages;
+        const unsigned id = there ? (unsigned)asked : 0u;
         const size_t off = (size_t)id * (page_bytes / 2) + ((head << ps_log) + (unsigned)(key & ((1 << ps_log) - 1))) * HD;
         const int bytes = __builtin_amdgcn_readfirstlane(there ? max(min(seen - key, 8), 0) * HD : 0);
         k_sc = load_const(k_scales, (size_t)id * Hkv + head);
@@ -259,48 +275,45 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
                      __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false)),
                      __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true))};
     };
-    auto commit = [&](unsigned char *st) __attribute__((always_inline)) {
+    auto commit = [&](unsigned char *st, int i) __attribute__((always_inline)) {
         const int l = lane_now(), r = 8 * wave + (l >> 3);
-#pragma unroll
-        for (int i = 0; i < CW / 2; ++i) {
-            *(u32x4 *)(st + k_off<HD>(r, (l & 7) * (CW / 2) + i)) = widen4(kc[2 * i], kc[2 * i + 1], k_sc);
-            *(u32x4 *)(st + VRING + v_off<HD>(r, (l & 7) * (CW / 2) + i)) = widen4(vc[2 * i], vc[2 * i + 1], v_sc);
-        }
+        *(u32x4 *)(st + k_off<HD>(r, (l & 7) * (CW / 2) + i)) = widen4(kc[2 * i], kc[2 * i + 1], k_sc);
+        *(u32x4 *)(st + VRING + v_off<HD>(r, (l & 7) * (CW / 2) + i)) = widen4(vc[2 * i], vc[2 * i + 1], v_sc);
     };
 
     // ---- a tile in two phases ----
     // M(j): the products, V^T P^T of tile j - 1 and K Q^T of tile j;  S(j): the softmax of tile j.  The two waves of a SIMD (wave
     // and wave + 4) are one phase apart, so that one's matrix instructions run under the other's exponentials; a barrier ends
-    // every phase: the early waves' M(j) is phase 2 j, the late ones' phase 2 j + 1.  In S(j) a wave asks for its part of tile
-    // j + 2, in the stage of tile j - 2, whose values the late waves read for the last time in phase 2 j - 1.  Tile j has
-    // to be there in phase 2 j: before the barrier ahead of it an early wave (at the end of S(j - 1)) waits for all but the
-    // tile asked for last, a late one (at the end of M(j - 1)) for all.
+    // every phase: the early waves' M(j) is phase 2 j, the late ones' phase 2 j + 1.  S is the longer phase, so the rest is M's: in
+    // M(j) a wave asks for its part of tile j + 2, in the stage of tile j - 2, whose values the late waves read for the last time in
+    // phase 2 j - 1.  Tile j has to be there in phase 2 j: before the barrier ahead of it an early wave (at the end of S(j - 1)) and a
+    // late one (at the end of M(j - 1)) waits for all but the tile asked for last.
     f32x16 s[2];
     bf16x8 pf[4];
     u32x4 vf[NDB][4];
     const bool late = wave >= 4;
     auto phase_end = [&](auto M, bool wait = true) __attribute__((always_inline)) {
         if (KIND != PAGED_BF16) {
-            if (decltype(M)::value) PD_TILE_LGKM0();     // codes written in S(j) are needed after the wave's M(j + 1)
-        } else if (!decltype(M)::value) {
+            if (decltype(M)::value) PD_TILE_LGKM0();     // codes written in M(j) are needed in M(j + 2)
+        } else if (!decltype(M)::value || (late && wait)) {
             PD_TILE_VMCNT(2 * LPW);
-        } else if (late && wait) {
-            PD_TILE_VMCNT(0);
         }
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+        if (decltype(M)::value) __builtin_amdgcn_s_setprio(0);
+        else __builtin_amdgcn_s_setprio(1);
         __builtin_amdgcn_sched_barrier(0);
     };
     int ring;                                        // offset of the stage of the products' tile
     auto stage = [&](int i) __attribute__((always_inline)) { return smem + ((ring + i * TILE) & (NST * TILE - 1)); };
-    auto ahead = [&]() __attribute__((always_inline)) {      // in S(j)
+    auto ahead = [&](unsigned char *st, int quarter) __attribute__((always_inline)) {      // in M(j): tile j + 2, into st
         if (KIND == PAGED_BF16) {
-            issue(stage(2));
-            ask();
+            if (quarter < LPW) issue(st, quarter, ids);
+            if (quarter == 3) ask(ids);
         } else {
-            commit(stage(2));
-            fetch();
-            ask_codes();
+            if (quarter < CW / 2) commit(st, quarter);
+            if (quarter == 2) fetch(ids[0]);
+            if (quarter == 3) ask_codes(ids[0]);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -395,19 +408,24 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
         __builtin_amdgcn_sched_barrier(0);
         load_v(st, 0);
         load_v(st, 1);
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    // the rest of V^T P^T out of st and, unless this was the last tile, K Q^T out of st_k: operands are requested a quarter ahead
-    auto products = [&](const unsigned char *st, const unsigned char *st_k, auto NEXT) __attribute__((always_inline)) {
         load_v(st, 2);
         load_v(st, 3);
         __builtin_amdgcn_sched_barrier(0);
+    };
+    // V^T P^T out of st and, unless this was the unit's last tile, K Q^T out of st_k, requested ahead; between the products what
+    // is asked for into st_next
+    auto products = [&](unsigned char *st_k, unsigned char *st_next, auto NEXT) __attribute__((always_inline)) {
         mul_v(0);
+        __builtin_amdgcn_sched_barrier(0);
+        ahead(st_next, 0);
         mul_v(1);
         __builtin_amdgcn_sched_barrier(0);
         if (decltype(NEXT)::value) load_k(st_k, 0);
         __builtin_amdgcn_sched_barrier(0);
+        ahead(st_next, 1);
         mul_v(2);
+        __builtin_amdgcn_sched_barrier(0);
+        ahead(st_next, 2);
         mul_v(3);
         __builtin_amdgcn_sched_barrier(0);
         if (decltype(NEXT)::value) {
@@ -418,6 +436,7 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
             mul_k(1);
             __builtin_amdgcn_sched_barrier(0);
         }
+        ahead(st_next, 3);                           // (scalar loads under way would have the products wait for all of their operands)
     };
     // A weight of 0 times a value that is infinite or NaN is NaN: such a value would reach rows that do not see it.  The results
     // tell: where one is not finite, the tiles are gone through again with the values in question taken out in LDS, and these
@@ -436,12 +455,21 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
         PD_TILE_LGKM0();
     };
     // ---- a unit ends: a lane holds one row's channels 32 db + 8 (r / 4) + 4 h + r % 4 ----
-    auto finish = [&]() __attribute__((always_inline)) {
-        const int r0 = PD_ITEM(item, r0), g = PD_ITEM(item, g), start = PD_ITEM(item, start), slot = PD_ITEM(item, slot);
+    struct Ending {
+        Unit u;
+        int slot, Hq;
+        uint16_t *out;
+        float *ml, *o;
+    };
+    auto ending_of = [&](int i) __attribute__((always_inline)) {
         const auto args = rare();
-        const int G = args->G, row = r0 + w0 + n;
-        const int rows = PD_ITEM(item, rows);
-        const bool ok = row < rows;
+        Ending e = {unit_of(i, args->G), PD_ITEM(i, slot), args->Hq, (uint16_t *)args->out, args->parts.ml, args->parts.o};
+        e.out += ((size_t)(e.u.start + e.u.tok) * e.Hq + e.u.head + e.u.rest) * HD;
+        return e;
+    };
+    auto finish = [&](const Ending &e) __attribute__((always_inline)) {
+        const Unit &u = e.u;
+        const bool ok = w0 + n < u.rows - u.r0;
         if (!clean) {
             float zero = 0.f;                        // (infinity or NaN) * 0 is NaN, and no sum removes it
 #pragma unroll
@@ -450,6 +478,8 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
                 for (int r = 0; r < 16; ++r) zero = fmaf(o[db][r], 0.f, zero);
             if (__any(ok && zero != 0.f) && lane == 0) atomicOr(&bad, 1u << item);
         } else {
+            const auto args = rare();
+            const int g = PD_ITEM(item, g);
             const int32_t *table = args->p.table + (size_t)PD_ITEM(item, seq) * args->p.width;
             const int end = min(t_hi * kTileKeys, PD_ITEM(item, seen));
 #pragma unroll 1
@@ -469,7 +499,7 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
             }
         }
         const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
-        if (slot < 0) {
+        if (e.slot < 0) {
             // halves of the wave trade registers, so that a lane has eight consecutive channels
             const float inv = limit <= 0 ? 0.f : 1.f / l_tot;
             u32x4 x[2 * NDB];
@@ -487,35 +517,34 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
                 }
             rows_swap16(x);
             rows_swap8(x);
-            uint16_t *op = (uint16_t *)args->out + 8 * rows_piece(lane_now());
-            const int Hq = args->Hq;
+            const int piece = 8 * rows_piece(lane_now());
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int row = r0 + row_of(i), tok = row / G;
-                uint16_t *at = op + ((size_t)(start + tok) * Hq + g * G + row - tok * G) * HD;
+                const int w = row_of(i), tok = u.token(w);
+                uint16_t *at = e.out + ((tok * e.Hq + w - tok * u.G) * HD + piece);      // (a unit's rows are not far apart)
 #pragma unroll
                 for (int k = 0; k < NDB / 2; ++k)
-                    if (row < rows) *(u32x4 *)(at + 64 * k) = x[4 * k + i];
+                    if (w < u.rows - u.r0) *(u32x4 *)(at + 64 * k) = x[4 * k + i];
             }
         } else {
-            const size_t to = (size_t)slot * kTileRows;
-            if (h == 0 && ok) *(float2 *)(args->parts.ml + (to + w0 + n) * 2) = make_float2(m_run, l_tot);
-            float *op = args->parts.o + to * HD + 4 * rows_piece(lane_now());
+            const size_t to = (size_t)e.slot * kTileRows;
+            if (h == 0 && ok) *(float2 *)(e.ml + (to + w0 + n) * 2) = make_float2(m_run, l_tot);
+            float *op = e.o + to * HD + 4 * rows_piece(lane_now());
 #pragma unroll
             for (int db = 0; db < NDB; db += NDB / 2) {
                 u32x4 x[2 * NDB];
 #pragma unroll
                 for (int i = 0; i < 2 * NDB; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[i][e] = __builtin_bit_cast(unsigned, (float)o[db + i / 4][4 * (i & 3) + e]);
+                    for (int c = 0; c < 4; ++c) x[i][c] = __builtin_bit_cast(unsigned, (float)o[db + i / 4][4 * (i & 3) + c]);
                 rows_swap16(x);
                 rows_swap8(x);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int row = row_of(i);
+                    const int w = row_of(i);
 #pragma unroll
                     for (int k = 0; k < NDB / 2; ++k)
-                        if (r0 + row < rows) *(u32x4 *)(op + row * HD + 32 * (db + k)) = x[4 * k + i];
+                        if (w < u.rows - u.r0) *(u32x4 *)(op + w * HD + 32 * (db + k)) = x[4 * k + i];
                 }
             }
         }
@@ -551,33 +580,47 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
             n_listed = min(part.to - first, kListed);
         }
         asm volatile("" : "+v"(n), "+v"(h));         // addresses are formed here, not kept from before a loop that rarely runs twice
-        load_q(0);
         page_of(0);
         rows_of(0);
         ring = 0;
+        load_q(0);
+        // all page numbers are asked for before the first is waited for
         if (KIND == PAGED_BF16) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                ask();
-                issue(smem + i * TILE);
-                settle_all();
-            }
-            ask();
-        } else {
+            int early[3][LPW];
 #pragma unroll
             for (int i = 0; i < 3; ++i) {
-                ask_codes();
-                fetch();
-                if (i < 2) commit(smem + i * TILE);
-                settle_all();
+                ask(early[i]);
+                settle(pg, page_of);
             }
-            ask_codes();
+            ask(ids);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+#pragma unroll
+                for (int x = 0; x < LPW; ++x) issue(smem + i * TILE, x, early[i]);
+                settle(at, rows_of);
+            }
+        } else {
+            int early[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                ask_codes(early[i]);
+                settle(pg, page_of);
+            }
+            ask_codes(ids[0]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                fetch(early[i]);
+#pragma unroll
+                for (int x = 0; x < CW / 2; ++x)
+                    if (i < 3) commit(smem + i * TILE, x);
+                settle(at, rows_of);
+            }
         }
         __builtin_amdgcn_sched_barrier(0);
-        begin(0);
+        begin(0, bounds_of(0));
         turn_q();
         if (tid == 0) bad = 0;
-        if (KIND == PAGED_BF16) PD_TILE_VMCNT(2 * LPW);
+        if (KIND == PAGED_BF16) PD_TILE_VMCNT(4 * LPW);
         PD_TILE_LGKM0();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -588,11 +631,10 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
             settle_all();
             renew();
             for (int left = min(t_hi - 1 - j, min(at.t_hi - at.j, pg.t_hi - pg.j)); left > 0; --left) {       // S(j), M(j + 1)
-                ahead();
                 softmax(j, stage(0));
                 phase_end(std::false_type{});
                 if (clean) clean_v(stage(1));
-                products(stage(0), stage(1), std::true_type{});
+                products(stage(1), stage(3), std::true_type{});
                 phase_end(std::true_type{});
                 ring = (ring + TILE) & (NST * TILE - 1);
                 ++j;
@@ -602,15 +644,17 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
             settle_all();
             // the unit's last tile: between its two products the next unit's rows take the place of these
             const bool more = item + 1 < n_listed;
-            load_q(min(item + 1, n_listed - 1));
-            ahead();
+            const int next = min(item + 1, n_listed - 1);
+            load_q(next);
             softmax(j, stage(0));
+            const Ending e = ending_of(item);
+            const Bounds x = bounds_of(next);
             if (more || !late) phase_end(std::false_type{});
-            products(stage(0), nullptr, std::false_type{});
-            if (KIND == PAGED_BF16 && late && more) PD_TILE_VMCNT(0);      // here, not for the stores
-            finish();
+            products(nullptr, stage(3), std::false_type{});
+            if (KIND == PAGED_BF16 && late) PD_TILE_VMCNT(2 * LPW);        // here, not for the stores
+            finish(e);
             if (!more) break;
-            begin(item + 1);
+            begin(next, x);
             turn_q();
             ring = (ring + TILE) & (NST * TILE - 1);
             first_scores();

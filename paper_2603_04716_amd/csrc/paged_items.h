@@ -166,7 +166,7 @@ constexpr int kCutTiles = 8;             // a unit of fewer tiles is never split
 struct PagedTilesItem {
     int seq, g, start, r0;               // sequence, kv head, first row of the sequence, first (token, head) row of the unit
     int rows, before, t_lo, t_hi;        // (token, head) rows of the sequence, position of its first row, tiles
-    int seen, slot, len, pad;            // keys that the unit sees; partial, or -1; positions of the sequence
+    int seen, slot, len, tok;            // keys that the unit sees; partial, or -1; positions of the sequence; token of row r0
 };
 struct PagedTilesSeq {
     long long at;                        // count and units ahead of the sequence
@@ -331,7 +331,7 @@ __device__ __forceinline__ void paged_tiles_list(const PagedAttnArgs &a, PagedTi
         const int k = first + lane, g = (k - q.unit) / s.units, i = k - q.unit - g * s.units, u = s.tile(i), seen = s.seen(a, u), tiles = s.tiles(seen);
         const int lo = k == part.from ? part.tile : 0, hi = k == part.to - 1 && part.tile_to ? part.tile_to : tiles;
         const int slot = lo > 0 ? 2 * part.w : hi < tiles ? 2 * part.w + 1 : -1;
-        sh.item[wave][lane] = PagedTilesItem{q.seq, g, q.start, u * R, s.rows, s.before, lo, hi, seen, slot, q.len, 0};
+        sh.item[wave][lane] = PagedTilesItem{q.seq, g, q.start, u * R, s.rows, s.before, lo, hi, seen, slot, q.len, u * R / a.G};
         if (wave == 0 && k == part.to - 1 && a.parts.desc) {
             int parts = 0;
             if (lo == 0 && hi < tiles) {
