@@ -312,8 +312,10 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
             if (quarter == 3) ask(ids);
         } else {
             if (quarter < CW / 2) commit(st, quarter);
-            if (quarter == 2) fetch(ids[0]);
-            if (quarter == 3) ask_codes(ids[0]);
+            if (quarter == 3) {
+                fetch(ids[0]);
+                ask_codes(ids[0]);
+            }
         }
         __builtin_amdgcn_sched_barrier(0);
     };
