@@ -335,3 +335,64 @@ def test_a_prompt_in_any_division_is_the_same_prompt(kind):
             want, weight, delta = P.attend(*c.host(), [0, n], [n], c.table_h, f64(q), hd ** -0.5)
             bound = attention_bound(kind, want, weight, delta, [n], [0, n], hd)
             assert (np.abs(f64(o) - want)[-m:] <= bound[-m:]).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("hq,hkv,hd,ps", [(64, 16, 64, 16), (16, 8, 128, 32)])
+def test_more_units_than_a_workgroup_lists(kind, hq, hkv, hd, ps):
+    """Hundreds of short chunks in one call, with a long one among them; then with infinities and NaN where nobody looks."""
+    rng = np.random.default_rng(19)
+    n = 5000 // hkv
+    seqs = [(int(a), int(a + b)) for a, b in zip(rng.integers(9, 20, n), rng.integers(0, 30, n))]
+    seqs[n // 3] = (200, 2600)
+    c = Paged(kind, hq, hkv, hd, ps, seqs, pad=5, seed=19)
+    clean = c.attend()
+    check(c, clean)
+    x = c.v.view(torch.uint8) if kind == "e4m3" else c.v
+    for b in range(0, n, 3):                                     # the last page's slots behind the sequence's end
+        m = c.lens_h[b]
+        if m % ps:
+            x[int(c.table_h[b, m // ps]), :, m % ps:] = 0x7F if kind == "e4m3" else float("inf")
+    assert torch.equal(c.attend(), clean)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_rows_about_the_border_of_the_kernels(kind):
+    """31 to 33 (token, head) rows, whole tiles of 256 and one more, in one call and with a length of zero."""
+    c = Paged(kind, 3, 3, 64, 16, [(31, 60), (32, 500), (33, 33), (256, 300), (257, 257), (255, 900), (40, 0)], seed=20)
+    check(c, c.attend())
+    c = Paged(kind, 8, 1, 128, 128, [(4, 900), (5, 900), (32, 200), (33, 4000), (64, 64)], pad=1, seed=21)
+    check(c, c.attend())
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_more_rows_than_positions(kind):
+    """Whole tiles of rows that see nothing are zeros, beside rows that see keys and sequences that hold none."""
+    c = Paged(kind, 4, 2, 128, 16, [(300, 20), (700, 300), (90, 0), (20, 900)], pad=2, seed=22)
+    check(c, c.attend())
+    got = c.attend()
+    assert (got[:280] == 0).all() and (got[300:700] == 0).all() and (got[1000:1090] == 0).all()
+    c = Paged(kind, 4, 2, 64, 64, [(50, 0), (1, 0), (300, 0)], seed=23)
+    assert (c.attend() == 0).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_prompts_of_one_length(kind):
+    """Equal prompts, whose tiles the workgroups share without splitting one, and so many rows that all have several."""
+    c = Paged(kind, 16, 4, 64, 64, [(1000, 1000), (1000, 1000), (1000, 1000)], seed=24)
+    check(c, c.attend())
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_a_value_that_is_not_a_number_in_a_split_unit(kind):
+    """A chunk behind a long past, whose keys many workgroups share: one NaN in the past makes its channel NaN in all rows, and no
+    other element changes."""
+    c = Paged(kind, 8, 2, 128, 32, [(40, 20000)], seed=25)
+    clean = c.attend()
+    check(c, clean)
+    x = c.v.view(torch.uint8) if kind == "e4m3" else c.v
+    x[int(c.table_h[0, 5000 // 32]), 1, 5000 % 32, 77] = 0x7F if kind == "e4m3" else float("nan")
+    got = c.attend()
+    hit = torch.zeros_like(got, dtype=torch.bool)
+    hit[:, 4:, 77] = True
+    assert torch.isnan(got[hit]).all() and torch.equal(got[~hit], clean[~hit])
