@@ -598,7 +598,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a, Paged
             store4((T *)a.out + ((size_t)(lo[i].z + tok) * a.Hq + head) * HD + 4 * d4, x);
         };
         if (parts <= kWavePartials) {
-            for (int r = 16 * (block % groups) + 4 * wave; r < rows; r += 16 * groups) {
+            for (int r = 16 * (block % groups) + 4 * ((wave + i) & 3); r < rows; r += 16 * groups) {      // units of few rows: each another wave
                 // 16 lanes have a row's weights
                 const int wr = min(r + (lane >> 4), rows - 1), wp = lane & 15;
                 const float2 f = *(const float2 *)(ml + (merge_at(min(wp, parts - 1)) * stride + wr) * 2);
