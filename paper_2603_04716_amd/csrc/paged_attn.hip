@@ -718,8 +718,8 @@ PagedAttnPlan paged_attn_plan(int kind, int hd, const PagedView &p, int Hq)
         t.rows = 256;
         t.rows_above = one ? 0 : kFewRows;
         t.rows_most = most;
-        t.least = 8;
-        const int64_t units = most_units(t.rows, t.rows_above, t.rows_most, p, G), parts = (max_len + 511) / 512;
+        t.least = 4;
+        const int64_t units = most_units(t.rows, t.rows_above, t.rows_most, p, G), parts = (max_len + 255) / 256;
         t.grid = (unsigned)std::min<int64_t>(kTileStreams, units * std::max<int64_t>(parts, 1));
         t.used = units > 0;
         t.merge = t.used && max_len > 448 && t.grid > 1;        // (a unit of fewer than eight tiles is never split)

@@ -265,7 +265,7 @@ __device__ __forceinline__ PagedTilesPart paged_tiles_part(const PagedAttnArgs &
     }
     if (rows > (float)a.p.n_rows) total = 0;         // the sequences' rows overlap: no such call, and nothing is done
     r.per = max((long long)(paged_quotient(total, W) + 1LL), (long long)a.least * TK * a.G);
-    r.margin = max((long long)kCutTiles / 2 * TK * a.G, r.per / 32);
+    r.margin = max((long long)kCutTiles / 2 * TK * a.G, r.per / 16);
     if (total == 0 || r.w * r.per >= total) return r;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
