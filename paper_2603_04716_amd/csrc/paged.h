@@ -72,13 +72,14 @@ struct PagedAttnArgs {
     float scale;
     int32_t rows_above, rows_most;   // this kernel's sequences: more (token, head) rows than the one, at most the other
     int32_t least;                   // fewest blocks (few rows) or tiles (many) of a workgroup
+    int32_t whole;                   // (few) no unit is split
     PagedParts parts;
 };
 // How one of the two kernels is launched, and its part of the workspace: from the host's fields of the call alone.
 struct PagedAttnPart {
     bool used, merge;                // launched at all; some of its units may be split
     int rows;                        // query rows of a unit
-    int rows_above, rows_most, least, merge_groups, merge_units;
+    int rows_above, rows_most, least, whole, merge_groups, merge_units;
     unsigned grid;
     int cap_units, cap_items;        // units to be merged and their partials: at most
     size_t off_desc, off_ml, off_o;

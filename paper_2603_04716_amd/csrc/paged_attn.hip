@@ -672,6 +672,11 @@ constexpr int kFewRows = 32;        // (token, head) rows of a sequence and kv h
 // Its workgroups: two on each of the 256 CUs.  64 sequences of 2000 positions take 97 us so, 100 us with half as many, and 100 us with
 // twice as many, whose partials are twice as many too (32 sequences of 4 rows: 66, 61 and 73 us).
 constexpr int kStreams = 512;
+// Most blocks that a table has room for up to which no unit is split, which saves the partials and the kernel that adds them up;
+// for fewer than 32 units, which leave most CUs idle, and for more.  8 kv heads, bf16, one sequence of 700 positions: 12.1 us so and
+// 12.9 us split, of 1000: 14.6 and 12.3 us; 64 sequences of up to 1000: 41 and 51 us, 256: 154 and 152 us.  (fp32, nine chunks of up to
+// 60 rows at up to 960 positions, 15 blocks: 25 and 16 us.)
+constexpr int kWholeBlocksFew = 6, kWholeBlocks = 8;
 constexpr int kTileStreams = 256;   // workgroups of the other kernel, each of which fills a CU
 constexpr int kStreamBlocks = 1;    // fewest blocks (a step for each wave) of one
 
@@ -706,9 +711,10 @@ PagedAttnPlan paged_attn_plan(int kind, int hd, const PagedView &p, int Hq)
         t.least = kStreamBlocks;
         const int64_t units = most_units(t.rows, 0, t.rows_most, p, G), block = kWaves * (kind == PAGED_F32 ? 16 : 32);
         const int64_t blocks = (max_len + block - 1) / block;
-        t.grid = (unsigned)std::min<int64_t>(kStreams, units * blocks);
+        t.whole = blocks <= (units < 32 ? kWholeBlocksFew : kWholeBlocks);
+        t.grid = (unsigned)std::min<int64_t>(kStreams, t.whole ? units : units * blocks);
         t.used = units > 0;
-        t.merge = t.used && blocks > 1 && t.grid > 1;
+        t.merge = t.used && !t.whole && blocks > 1 && t.grid > 1;
         if (t.merge) {
             t.cap_units = (int)t.grid;
             t.cap_items = 2 * (int)t.grid;
@@ -743,7 +749,7 @@ PagedAttnPlan paged_attn_plan(int kind, int hd, const PagedView &p, int Hq)
 
 static PagedAttnArgs part_args(PagedAttnArgs a, const PagedAttnPart &t, char *ws)
 {
-    a.rows_above = t.rows_above; a.rows_most = t.rows_most; a.least = t.least;
+    a.rows_above = t.rows_above; a.rows_most = t.rows_most; a.least = t.least; a.whole = t.whole;
     if (!t.merge) return a;
     a.parts.desc = (int32_t *)(ws + t.off_desc);
     a.parts.ml = (float *)(ws + t.off_ml);

@@ -118,8 +118,9 @@ __device__ __forceinline__ PagedStream paged_stream(const PagedAttnArgs &a, Page
     }
     PagedStream st = {BASE, 0, 1, 0, r};
     if (rows > (float)a.p.n_rows) return st;         // the sequences' rows overlap: no such call, and nothing is done
+    if (a.whole) st.gran = 1 << 30;
     // larger blocks where their number would not fit an int32 (a sequence without keys is a block too, hence the margin)
-    for (float x = blocks * (float)a.p.Hkv; x > (float)(1 << 29); x *= 0.5f) st.gran *= 2;
+    else for (float x = blocks * (float)a.p.Hkv; x > (float)(1 << 29); x *= 0.5f) st.gran *= 2;
     int own = 0;
     paged_each(a, r, [&](int, int, int n_rows, int len) { own += a.p.Hkv * paged_units<R>(a, n_rows) * paged_chunks(len, st.gran); });
     const int own_to = wave_scan(own);
