@@ -231,7 +231,8 @@ typedef struct {
  * (an empty slot of a fixed-size batch: length 0); attention gives such a row zeros.
  * The arrays' contents are not checked on the host, and none of them makes a call touch memory outside its tensors: starts
  * outside 0 .. n_rows and lengths outside 0 .. table_width * page_size count as the nearest bound, a position whose page number
- * lies outside 0 .. n_pages - 1 is not stored and reads as zeros, and where sequences' rows overlap attention does nothing.
+ * lies outside 0 .. n_pages - 1 is not stored and reads as zeros, and where sequences have more than n_rows rows together, as starts
+ * that decrease can make them, attention does nothing (other such starts leave a row that two sequences own with one's results).
  * table_width * page_size is at most 2^30.
  */
 typedef struct {
@@ -279,7 +280,7 @@ pd_status pd_paged_append(const pd_paged_kv *kv, const pd_paged_seqs *seqs, cons
  * own keys and values are read from the cache like all others (pd_paged_append first).  One row per sequence is a decode
  * step, several are drafted tokens or a chunk, lens equal to the rows a whole prompt, in any mixture.
  * q [n_rows, n_q_heads, head_dim] with a row stride in elements as above; out [n_rows, n_q_heads, head_dim] contiguous, 16-byte
- * aligned.  Scores, softmax and sums in fp32; in bf16 the exponentials are rounded to bf16 before they weigh the values.
+ * aligned; it does not overlap q or the pages.  Scores, softmax and sums in fp32; in bf16 the exponentials are rounded to bf16 before they weigh the values.
  * Results do not depend on what else is in a page: unused slots, later positions and infinities or NaN in them.
  * A row without a visible position gets zeros.
  * workspace: device memory, 16-byte aligned, of at least pd_paged_attention_workspace bytes for the same host-side sizes

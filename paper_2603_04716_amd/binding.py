@@ -324,10 +324,13 @@ def make_paged_kv(k_pages, v_pages, k_scales=None, v_scales=None):
     for t in (k_scales, v_scales):
         if (t is not None) != codes or (codes and (t.dtype != torch.float32 or t.shape != k_pages.shape[:2] or not t.is_contiguous())):
             raise ValueError("make_paged_kv: codes, and only they, have scales: contiguous float32 [n_pages, n_kv_heads]")
+    devices = {t.get_device() for t in (k_pages, v_pages, k_scales, v_scales) if t is not None}
+    if len(devices) > 1:
+        raise ValueError("make_paged_kv: all tensors are on one device")
     n, h, ps, hd = k_pages.shape
     kv = pd_paged_kv(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr() if codes else None, v_scales.data_ptr() if codes else None,
                      n, ps, h, hd, PD_F32 if k_pages.dtype == torch.float32 else PD_BF16, int(codes))
-    kv.tensors = (k_pages, v_pages, k_scales, v_scales)
+    kv.tensors, kv.device = (k_pages, v_pages, k_scales, v_scales), devices.pop()
     return kv
 
 
@@ -337,13 +340,25 @@ def make_paged_seqs(lens, page_table, row_starts=None, n_rows=None):
     for t in (lens, page_table, row_starts):
         if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
             raise ValueError("make_paged_seqs: contiguous int32 tensors")
+    devices = {t.get_device() for t in (lens, page_table, row_starts) if t is not None}
+    if len(devices) > 1:
+        raise ValueError("make_paged_seqs: all tensors are on one device")
     n = lens.shape[0]
     if page_table.dim() != 2 or page_table.shape[0] != n or (row_starts is not None and (row_starts.shape != (n + 1,) or n_rows is None)):
         raise ValueError("make_paged_seqs: page_table [n_seqs, table_width], row_starts [n_seqs + 1] together with n_rows")
     seqs = pd_paged_seqs(n, n if n_rows is None else int(n_rows), None if row_starts is None else row_starts.data_ptr(), lens.data_ptr(),
                          page_table.data_ptr(), page_table.shape[1])
-    seqs.tensors = (lens, page_table, row_starts)
+    seqs.tensors, seqs.device = (lens, page_table, row_starts), devices.pop()
     return seqs
+
+
+def _paged_stream(who, kv, seqs, *tensors):
+    """The current stream, whose device has to hold all tensors of a call."""
+    stream = torch.cuda.current_stream()
+    here = stream.device_index
+    if kv.device != here or seqs.device != here or any(t.get_device() != here for t in tensors):
+        raise ValueError(f"{who}: all tensors are on the current device")
+    return C.c_void_p(stream.cuda_stream)
 
 
 def _paged_stride(who, t, kv, seqs, heads):
@@ -358,12 +373,15 @@ def _paged_stride(who, t, kv, seqs, heads):
 def pd_paged_append(kv, seqs, k, v, rope_base=0.0, q=None, q_out=None):
     """k, v [n_rows, n_kv_heads, head_dim] into the pages of kv; q [n_rows, n_q_heads, head_dim] rotated into q_out."""
     who, h = "pd_paged_append", kv.n_kv_heads
+    if (q is None) != (q_out is None):
+        raise ValueError(f"{who}: q and q_out belong together")
     rows = pd_paged_rows(k.data_ptr(), v.data_ptr(), None, None, _paged_stride(who, k, kv, seqs, h), _paged_stride(who, v, kv, seqs, h), 0, 0,
                          0, rope_base)
     if q is not None:
         rows.q, rows.q_out, rows.n_q_heads = q.data_ptr(), q_out.data_ptr(), q.shape[1]
         rows.q_stride, rows.q_out_stride = _paged_stride(who, q, kv, seqs, q.shape[1]), _paged_stride(who, q_out, kv, seqs, q.shape[1])
-    _check(lib.pd_paged_append(C.byref(kv), C.byref(seqs), C.byref(rows), _stream()))
+    stream = _paged_stream(who, kv, seqs, k, v) if q is None else _paged_stream(who, kv, seqs, k, v, q, q_out)
+    _check(lib.pd_paged_append(C.byref(kv), C.byref(seqs), C.byref(rows), stream))
 
 
 def pd_paged_attention_workspace(kv, seqs, n_q_heads):
@@ -375,12 +393,14 @@ def pd_paged_attention_workspace(kv, seqs, n_q_heads):
 
 def pd_paged_attention(kv, seqs, q, out, workspace, scale=None):
     """out [n_rows, n_q_heads, head_dim] (contiguous) = attention of q over the pages; scale: 1 / sqrt(head_dim) by default."""
-    stride = _paged_stride("pd_paged_attention", q, kv, seqs, q.shape[1])
-    if out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
-        raise ValueError("pd_paged_attention: out is a contiguous tensor like q")
+    who = "pd_paged_attention"
+    stride = _paged_stride(who, q, kv, seqs, q.shape[1])
+    if out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous() or not workspace.is_contiguous():
+        raise ValueError(f"{who}: out is a contiguous tensor like q, the workspace a contiguous tensor")
     _check(lib.pd_paged_attention(C.byref(kv), C.byref(seqs), q.data_ptr(), stride, q.shape[1],
                                   kv.head_dim ** -0.5 if scale is None else scale, out.data_ptr(),
-                                  workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
+                                  workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                  _paged_stream(who, kv, seqs, q, out, workspace)))
     return out
 
 

@@ -16,6 +16,9 @@
 // channel per lane.  A lane therefore loads hd / 16 channels of its eight keys and swaps halves of registers
 // (v_perm_b32, one per register), which takes no LDS and no lane crossing; accumulator c of a lane is then channel
 // (hd / 16) m + c of the matrix row m, 32 (hd 128) neighbouring channels per lane in all.
+//
+// Measured, 32 heads on 8 of 128 channels, one row per sequence: 64 sequences of 100 to 8000 positions 170 us or 5.7 TB/s, one of 131000
+// 92 us or 5.8 TB/s, 256 of 1500 to 2600 on E4M3 pages 192 us or 5.5 TB/s, and 5 us each for the partials.
 #include <string.h>
 
 #include <algorithm>

@@ -396,3 +396,25 @@ def test_a_value_that_is_not_a_number_in_a_split_unit(kind):
     hit = torch.zeros_like(got, dtype=torch.bool)
     hit[:, 4:, 77] = True
     assert torch.isnan(got[hit]).all() and torch.equal(got[~hit], clean[~hit])
+
+
+def test_tensors_elsewhere_are_refused():
+    c = Paged("bf16", 4, 2, 64, 16, [(2, 20)], seed=26)
+    q, k, v = c.parts()
+    host = torch.zeros(2, 4, 64, dtype=torch.bfloat16)
+    ws = c.workspace()
+    for bad in ((host, torch.zeros_like(c.q), ws), (c.q, host, ws), (c.q, torch.zeros_like(c.q), ws.cpu())):
+        with pytest.raises(ValueError):
+            pd.pd_paged_attention(c.kv, c.seqs, *bad)
+    with pytest.raises(ValueError):
+        pd.pd_paged_append(c.kv, c.seqs, k.cpu(), v)
+    with pytest.raises(ValueError):
+        pd.pd_paged_append(c.kv, c.seqs, k, v, 0.0, q, host)
+    with pytest.raises(ValueError):
+        pd.pd_paged_append(c.kv, c.seqs, k, v, 0.0, q)
+    with pytest.raises(ValueError):
+        pd.pd_paged_attention(pd.make_paged_kv(c.k.cpu(), c.v.cpu()), c.seqs, c.q, torch.zeros_like(c.q), ws)
+    with pytest.raises(ValueError):
+        pd.make_paged_kv(c.k, c.v.cpu())
+    with pytest.raises(ValueError):
+        pd.make_paged_seqs(c.lens, c.table.cpu())
