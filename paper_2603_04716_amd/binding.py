@@ -331,6 +331,7 @@ def make_paged_kv(k_pages, v_pages, k_scales=None, v_scales=None):
     kv = pd_paged_kv(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr() if codes else None, v_scales.data_ptr() if codes else None,
                      n, ps, h, hd, PD_F32 if k_pages.dtype == torch.float32 else PD_BF16, int(codes))
     kv.tensors, kv.device = (k_pages, v_pages, k_scales, v_scales), devices.pop()
+    kv.row_type, kv.heads, kv.hd = torch.float32 if k_pages.dtype == torch.float32 else torch.bfloat16, h, hd      # (for the checks of a call)
     return kv
 
 
@@ -348,39 +349,49 @@ def make_paged_seqs(lens, page_table, row_starts=None, n_rows=None):
         raise ValueError("make_paged_seqs: page_table [n_seqs, table_width], row_starts [n_seqs + 1] together with n_rows")
     seqs = pd_paged_seqs(n, n if n_rows is None else int(n_rows), None if row_starts is None else row_starts.data_ptr(), lens.data_ptr(),
                          page_table.data_ptr(), page_table.shape[1])
-    seqs.tensors, seqs.device = (lens, page_table, row_starts), devices.pop()
+    seqs.tensors, seqs.device, seqs.rows = (lens, page_table, row_starts), devices.pop(), seqs.n_rows
     return seqs
 
 
-def _paged_stream(who, kv, seqs, *tensors):
+def _paged_stream(who, kv, seqs, tensors):
     """The current stream, whose device has to hold all tensors of a call."""
     stream = torch.cuda.current_stream()
     here = stream.device_index
-    if kv.device != here or seqs.device != here or any(t.get_device() != here for t in tensors):
+    if kv.device != here or seqs.device != here:
         raise ValueError(f"{who}: all tensors are on the current device")
-    return C.c_void_p(stream.cuda_stream)
+    for t in tensors:
+        if t.get_device() != here:
+            raise ValueError(f"{who}: all tensors are on the current device")
+    return stream.cuda_stream
 
 
-def _paged_stride(who, t, kv, seqs, heads):
+def _paged_stride(who, t, kv, rows, heads):
     """Row stride of t [n_rows, heads, head_dim] whose rows hold their heads next to each other."""
-    hd = kv.head_dim
-    if (t.dtype != (torch.float32 if kv.dtype == PD_F32 else torch.bfloat16) or t.dim() != 3 or t.shape != (seqs.n_rows, heads, hd)
-            or (t.stride(2) != 1 or (heads > 1 and t.stride(1) != hd)) and t.numel() > 0):
-        raise ValueError(f"{who}: tensors are [n_rows, heads, head_dim] in the cache's row type, the heads of a row next to each other")
-    return t.stride(0) if seqs.n_rows > 1 else heads * hd
+    hd = kv.hd
+    if t.dtype is not kv.row_type or t.shape != (rows, heads, hd):
+        raise ValueError(f"{who}: tensors are [n_rows, heads, head_dim] in the cache's row type")
+    row, head, one = t.stride()
+    if (one != 1 or (heads > 1 and head != hd)) and rows > 0:
+        raise ValueError(f"{who}: the heads of a row lie next to each other")
+    return row if rows > 1 else heads * hd
 
 
 def pd_paged_append(kv, seqs, k, v, rope_base=0.0, q=None, q_out=None):
     """k, v [n_rows, n_kv_heads, head_dim] into the pages of kv; q [n_rows, n_q_heads, head_dim] rotated into q_out."""
-    who, h = "pd_paged_append", kv.n_kv_heads
-    if (q is None) != (q_out is None):
-        raise ValueError(f"{who}: q and q_out belong together")
-    rows = pd_paged_rows(k.data_ptr(), v.data_ptr(), None, None, _paged_stride(who, k, kv, seqs, h), _paged_stride(who, v, kv, seqs, h), 0, 0,
-                         0, rope_base)
-    if q is not None:
-        rows.q, rows.q_out, rows.n_q_heads = q.data_ptr(), q_out.data_ptr(), q.shape[1]
-        rows.q_stride, rows.q_out_stride = _paged_stride(who, q, kv, seqs, q.shape[1]), _paged_stride(who, q_out, kv, seqs, q.shape[1])
-    stream = _paged_stream(who, kv, seqs, k, v) if q is None else _paged_stream(who, kv, seqs, k, v, q, q_out)
+    who, n, h = "pd_paged_append", seqs.rows, kv.heads
+    strides = _paged_stride(who, k, kv, n, h), _paged_stride(who, v, kv, n, h)
+    if q is None:
+        if q_out is not None:
+            raise ValueError(f"{who}: q and q_out belong together")
+        rows = pd_paged_rows(k.data_ptr(), v.data_ptr(), None, None, *strides, 0, 0, 0, rope_base)
+        stream = _paged_stream(who, kv, seqs, (k, v))
+    else:
+        if q_out is None or q.dim() != 3:
+            raise ValueError(f"{who}: q [n_rows, n_q_heads, head_dim] and q_out belong together")
+        hq = q.shape[1]
+        rows = pd_paged_rows(k.data_ptr(), v.data_ptr(), q.data_ptr(), q_out.data_ptr(), *strides, _paged_stride(who, q, kv, n, hq),
+                             _paged_stride(who, q_out, kv, n, hq), hq, rope_base)
+        stream = _paged_stream(who, kv, seqs, (k, v, q, q_out))
     _check(lib.pd_paged_append(C.byref(kv), C.byref(seqs), C.byref(rows), stream))
 
 
@@ -394,13 +405,15 @@ def pd_paged_attention_workspace(kv, seqs, n_q_heads):
 def pd_paged_attention(kv, seqs, q, out, workspace, scale=None):
     """out [n_rows, n_q_heads, head_dim] (contiguous) = attention of q over the pages; scale: 1 / sqrt(head_dim) by default."""
     who = "pd_paged_attention"
-    stride = _paged_stride(who, q, kv, seqs, q.shape[1])
+    if q.dim() != 3:
+        raise ValueError(f"{who}: q is [n_rows, n_q_heads, head_dim]")
+    stride = _paged_stride(who, q, kv, seqs.rows, q.shape[1])
     if out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous() or not workspace.is_contiguous():
         raise ValueError(f"{who}: out is a contiguous tensor like q, the workspace a contiguous tensor")
     _check(lib.pd_paged_attention(C.byref(kv), C.byref(seqs), q.data_ptr(), stride, q.shape[1],
                                   kv.head_dim ** -0.5 if scale is None else scale, out.data_ptr(),
                                   workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                  _paged_stream(who, kv, seqs, q, out, workspace)))
+                                  _paged_stream(who, kv, seqs, (q, out, workspace))))
     return out
 
 
