@@ -418,3 +418,13 @@ def test_tensors_elsewhere_are_refused():
         pd.make_paged_kv(c.k, c.v.cpu())
     with pytest.raises(ValueError):
         pd.make_paged_seqs(c.lens, c.table.cpu())
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("hq,hkv", [(300, 1), (1024, 1), (99, 3)])
+def test_large_groups(kind, hq, hkv):
+    """A token's heads fill a tile of rows, or several."""
+    c = Paged(kind, hq, hkv, 64, 16, [(1, 90), (1, 700), (1, 0)], seed=27, starts=False)
+    check(c, c.attend())
+    c = Paged(kind, hq, hkv, 64, 16, [(3, 90), (1, 900), (2, 1), (7, 7)], pad=1, seed=28)
+    check(c, c.attend())
