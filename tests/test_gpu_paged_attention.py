@@ -428,3 +428,45 @@ def test_large_groups(kind, hq, hkv):
     check(c, c.attend())
     c = Paged(kind, hq, hkv, 64, 16, [(3, 90), (1, 900), (2, 1), (7, 7)], pad=1, seed=28)
     check(c, c.attend())
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_chunks_replayed_from_a_graph(kind):
+    """A captured call of chunks, drafts and single rows, replayed while starts, lengths and page numbers change on the device: each replay
+    equals the eager call, with eager work between the replays."""
+    steps = [[(100, 300), (1, 700), (9, 9), (40, 1500)], [(1, 301), (140, 840), (5, 14), (4, 1504)], [(0, 301), (1, 841), (149, 163), (0, 0)]]
+    c = Paged(kind, 8, 2, 128, 32, [(n, 1600) for n in (50, 50, 25, 25)], seed=29)
+    out = torch.zeros_like(c.q)
+    ws = c.workspace()
+    k, v = c.parts()[1:]
+    pages = [t.clone() for t in (c.k, c.v, c.ks, c.vs) if t is not None]
+
+    def call(q_out, out):
+        pd.pd_paged_append(c.kv, c.seqs, k, v, 10000.0, c.q, q_out)
+        pd.pd_paged_attention(c.kv, c.seqs, q_out, out, ws)
+
+    def reset(step):
+        for t, kept in zip([t for t in (c.k, c.v, c.ks, c.vs) if t is not None], pages):
+            t.copy_(kept)
+        c.row_starts.copy_(torch.tensor([0] + list(np.cumsum([n for n, _ in step])), dtype=torch.int32))
+        c.lens.copy_(torch.tensor([m for _, m in step], dtype=torch.int32))
+        c.table.copy_(c.table[[1, 2, 3, 0]])
+
+    q_out = torch.zeros_like(c.q)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        call(q_out, out)
+    for i in range(6):
+        reset(steps[i % 3])
+        out.fill_(7.0)
+        graph.replay()
+        got, got_k = out.clone(), c.k.clone()
+        table = c.table.clone()
+        reset(steps[i % 3])
+        c.table.copy_(table)
+        eager_q, eager = torch.zeros_like(c.q), torch.full_like(out, 7.0)
+        call(eager_q, eager)
+        torch.cuda.synchronize()
+        assert torch.equal(got, eager) and torch.equal(got_k.view(torch.uint8), c.k.view(torch.uint8)), i
+        assert torch.isfinite(eager.float()).all()
