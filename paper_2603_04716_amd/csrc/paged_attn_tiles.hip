@@ -294,7 +294,7 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
     // ---- a tile in two phases ----
     // M(j): the products, V^T P^T of tile j - 1 and K Q^T of tile j;  S(j): the softmax of tile j.  The two waves of a SIMD (wave
     // and wave + 4) are one phase apart, so that one's matrix instructions run under the other's exponentials; a barrier ends
-    // every phase: the early waves' M(j) is phase 2 j, the late ones' phase 2 j + 1.  S is the longer phase, so the rest is M's: in
+    // every phase: the early waves' M(j) is phase 2 j, the late ones' phase 2 j + 1.  What is asked for ahead is M's, between the products: in
     // M(j) a wave asks for its part of tile j + 2, in the stage of tile j - 2, whose values the late waves read for the last time in
     // phase 2 j - 1.  Tile j has to be there in phase 2 j: before the barrier ahead of it an early wave (at the end of S(j - 1)) and a
     // late one (at the end of M(j - 1)) waits for all but the tile asked for last.
