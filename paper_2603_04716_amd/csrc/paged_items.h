@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "paged.h"
+#include "paged_division.h"
 
 namespace pd {
 
@@ -154,17 +155,8 @@ __device__ __forceinline__ void paged_locate(const PagedAttnArgs &a, const Paged
 }
 
 // ---- many rows: bound by the matrix pipe; a unit's tiles of keys are what its last row sees ---------------------------------
-//
-// Row tile u of a sequence is counted with G (kUnitKeys + before) + R (u + 1), G times the keys that it sees and those that going from one
-// unit to the next takes the time of; inside a unit the count is proportional to its tiles.  The units of a sequence and kv head are
-// taken from both ends in turn (the last row tile, the first, the last but one, ..), which makes all pairs count the same: what is
-// ahead of a unit has a closed form, and where the parts hold whole pairs, as those of equal prompts mostly do, nothing is split.
-// A border closer than `margin` to an end of its unit moves there: a partial of few tiles costs more than the
-// unevenness.  Every workgroup finds the same cut for a border, and as tiles count less than `per` each, cuts inside a unit are
-// different tiles.  Of kUnitKeys 192, 256 and 384 a call of twelve chunks of 1 to 700 tokens behind up to 6000 takes 308, 295 and 299 us,
-// with margins of an eighth, a 16th and a 32nd of a part 311, 292 and 295 us.
-constexpr int kUnitKeys = 256, kListed = 16;
-constexpr int kCutTiles = 8;             // a unit of fewer tiles is never split
+// (how it is divided: paged_division.h)
+constexpr int kListed = 16;
 struct PagedTilesItem {
     int seq, g, start, r0;               // sequence, kv head, first row of the sequence, first (token, head) row of the unit
     int rows, before, t_lo, t_hi;        // (token, head) rows of the sequence, position of its first row, tiles
@@ -173,9 +165,6 @@ struct PagedTilesItem {
 struct PagedTilesSeq {
     long long at;                        // count and units ahead of the sequence
     int unit, seq, start, rows, len, pad;
-};
-struct PagedCut {
-    int unit, tile;
 };
 template <int NT>
 struct PagedTilesShared {
@@ -193,35 +182,11 @@ struct PagedTilesPart {
     int tile, tile_to;
     PagedOwn own;
 };
-// a / b of numbers below 2^53, by way of double: a tenth of the instructions of the compiler's 64-bit division
-__device__ __forceinline__ int paged_quotient(long long a, long long b)
-{
-    int q = (int)((double)a / (double)b);
-    if (a - q * b < 0) --q;
-    if (a - q * b >= b) ++q;
-    return q;
-}
 template <int R, int TK>
-struct PagedUnits {                      // of a sequence and kv head
-    int units, rows, before;
-    long long each, pair, all;           // each + R (u + 1): count of row tile u; count of a pair and of all units
-    __device__ __forceinline__ PagedUnits(const PagedAttnArgs &a, int n_rows, int len)
-    {
-        units = paged_units<R>(a, n_rows);
-        rows = n_rows * a.G;
-        before = len - n_rows;
-        each = (long long)a.G * (kUnitKeys + max(before, 0));
-        pair = 2 * each + (long long)R * (units + 1);
-        all = ahead(units);
-    }
-    __device__ __forceinline__ int tile(int i) const { return i & 1 ? i >> 1 : units - 1 - (i >> 1); }      // row tile of unit i
-    __device__ __forceinline__ long long count(int u) const { return each + (long long)R * (u + 1); }
-    __device__ __forceinline__ long long ahead(int i) const { return (i >> 1) * pair + (i & 1 ? count(tile(i - 1)) : 0); }
-    __device__ __forceinline__ int seen(const PagedAttnArgs &a, int u) const { return max(before + (min(R * (u + 1), rows) - 1) / a.G + 1, 0); }
-    __device__ __forceinline__ int tiles(int seen) const { return max((seen + TK - 1) / TK, 1); }
-    // (more rows than positions: the count says too little about the tiles)
-    __device__ __forceinline__ bool whole(int tiles) const { return tiles < kCutTiles || before < 0; }
-};
+__device__ __forceinline__ PagedUnits<R, TK> paged_units_of(const PagedAttnArgs &a, int n_rows, int len)
+{
+    return PagedUnits<R, TK>(paged_units<R>(a, n_rows), n_rows, len, a.G);
+}
 template <int R, int TK, int NT>
 __device__ __forceinline__ PagedTilesPart paged_tiles_part(const PagedAttnArgs &a, PagedTilesShared<NT> &sh)
 {
@@ -232,7 +197,7 @@ __device__ __forceinline__ PagedTilesPart paged_tiles_part(const PagedAttnArgs &
     int units = 0;
     float rows = 0.f;                    // exact up to 2^24, which no call has more of
     paged_each(a, r.own, [&](int, int, int n_rows, int len) {
-        const PagedUnits<R, TK> s(a, n_rows, len);
+        const PagedUnits<R, TK> s = paged_units_of<R, TK>(a, n_rows, len);
         count += Hkv * s.all;
         units += Hkv * s.units;
         rows += (float)n_rows;
@@ -266,8 +231,8 @@ __device__ __forceinline__ PagedTilesPart paged_tiles_part(const PagedAttnArgs &
         rows += sh.rows[w];
     }
     if (rows > (float)a.p.n_rows) total = 0;         // the sequences' rows overlap: no such call, and nothing is done
-    r.per = max((long long)(paged_quotient(total, W) + 1LL), (long long)a.least * TK * a.G);
-    r.margin = max((long long)kCutTiles / 2 * TK * a.G, r.per / 16);
+    r.per = paged_part_count<TK>(total, W, a.least, a.G);
+    r.margin = paged_margin<TK>(r.per, a.G);
     if (total == 0 || r.w * r.per >= total) return r;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -276,7 +241,7 @@ __device__ __forceinline__ PagedTilesPart paged_tiles_part(const PagedAttnArgs &
         long long at = r.first;
         int unit = r.first_units;
         paged_each(a, r.own, [&](int b, int start, int n_rows, int len) {
-            const PagedUnits<R, TK> s(a, n_rows, len);
+            const PagedUnits<R, TK> s = paged_units_of<R, TK>(a, n_rows, len);
             if (border >= at && border < at + Hkv * s.all) sh.border[i] = PagedTilesSeq{at, unit, b, start, n_rows, len, 0};
             at += Hkv * s.all;
             unit += Hkv * s.units;
@@ -287,22 +252,9 @@ __device__ __forceinline__ PagedTilesPart paged_tiles_part(const PagedAttnArgs &
     const long long border = (r.w + (lane & 1)) * r.per;
     if (border < total) {
         const PagedTilesSeq q = sh.border[lane & 1];
-        const PagedUnits<R, TK> s(a, q.rows, q.len);
-        long long y = border - q.at;
-        const int g = paged_quotient(y, s.all);
-        y -= g * s.all;
-        int i = 2 * paged_quotient(y, s.pair);
-        y -= (i >> 1) * s.pair;
-        const long long first_of_pair = s.count(s.tile(i));
-        if (i + 1 < s.units && y >= first_of_pair) {
-            ++i;
-            y -= first_of_pair;
-        }
-        const long long of = s.count(s.tile(i));
-        const int tiles = s.tiles(s.seen(a, s.tile(i)));
-        const bool inside = !s.whole(tiles) && y >= r.margin && y <= of - r.margin;
-        const bool next = !inside && 2 * y >= of;
-        cut = PagedCut{q.unit + g * s.units + i + next, inside ? min(max((int)((double)y * tiles / (double)of), 1), tiles - 1) : 0};
+        const PagedUnits<R, TK> s = paged_units_of<R, TK>(a, q.rows, q.len);
+        cut = s.cut(border - q.at, r.margin);
+        cut.unit += q.unit;
     }
     r.from = __builtin_amdgcn_readlane(cut.unit, 0);
     r.tile = __builtin_amdgcn_readlane(cut.tile, 0);
@@ -321,7 +273,7 @@ __device__ __forceinline__ void paged_tiles_list(const PagedAttnArgs &a, PagedTi
     __syncthreads();
     if (unit < end)
         paged_each(a, part.own, [&](int b, int start, int n_rows, int len) {
-            const PagedUnits<R, TK> s(a, n_rows, len);
+            const PagedUnits<R, TK> s = paged_units_of<R, TK>(a, n_rows, len);
             for (int k = max(first, unit); k < min(end, unit + Hkv * s.units); ++k) sh.of[k - first] = PagedTilesSeq{at, unit, b, start, n_rows, len, 0};
             unit += Hkv * s.units;
             at += Hkv * s.all;
@@ -329,8 +281,8 @@ __device__ __forceinline__ void paged_tiles_list(const PagedAttnArgs &a, PagedTi
     __syncthreads();
     if (first + lane < end) {
         const PagedTilesSeq q = sh.of[lane];
-        const PagedUnits<R, TK> s(a, q.rows, q.len);
-        const int k = first + lane, g = (k - q.unit) / s.units, i = k - q.unit - g * s.units, u = s.tile(i), seen = s.seen(a, u), tiles = s.tiles(seen);
+        const PagedUnits<R, TK> s = paged_units_of<R, TK>(a, q.rows, q.len);
+        const int k = first + lane, g = (k - q.unit) / s.units, i = k - q.unit - g * s.units, u = s.tile(i), seen = s.seen(u), tiles = s.tiles(seen);
         const int lo = k == part.from ? part.tile : 0, hi = k == part.to - 1 && part.tile_to ? part.tile_to : tiles;
         const int slot = lo > 0 ? 2 * part.w : hi < tiles ? 2 * part.w + 1 : -1;
         sh.item[wave][lane] = PagedTilesItem{q.seq, g, q.start, u * R, s.rows, s.before, lo, hi, seen, slot, q.len, u * R / a.G};
@@ -338,7 +290,7 @@ __device__ __forceinline__ void paged_tiles_list(const PagedAttnArgs &a, PagedTi
             int parts = 0;
             if (lo == 0 && hi < tiles) {
                 const long long u0 = q.at + g * s.all + s.ahead(i), u1 = u0 + s.count(u);
-                parts = 2 + paged_quotient(u1 - part.margin, part.per) - paged_quotient(u0 + part.margin + part.per - 1, part.per);
+                parts = paged_parts(u0, u1, part.margin, part.per);
             }
             paged_describe(a, part.w, slot, parts, q.start, u * R, s.rows, g, s.before);
         }
