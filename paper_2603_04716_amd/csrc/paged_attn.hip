@@ -209,6 +209,7 @@ struct Step<PAGED_E4M3, HD> : Step16<Step<PAGED_E4M3, HD>, HD> {
     {
 #pragma unroll
         for (int t = 0; t < HD / 64; ++t) k[kb][t] = u32x4{0u, 0u, 0u, 0u};
+        ks[kb] = vs[kb] = 1.f;                       // (the scale that was loaded is another page's, and may be no number)
     }
     __device__ __forceinline__ void clear_value(int i)
     {

@@ -263,8 +263,12 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
         const unsigned id = there ? (unsigned)asked : 0u;
         const size_t off = (size_t)id * (page_bytes / 2) + ((head << ps_log) + (unsigned)(key & ((1 << ps_log) - 1))) * HD;
         const int bytes = __builtin_amdgcn_readfirstlane(there ? max(min(seen - key, 8), 0) * HD : 0);
-        k_sc = load_const(k_scales, (size_t)id * Hkv + head);
-        v_sc = load_const(v_scales, (size_t)id * Hkv + head);
+        // (a page that is not there has no scale, and any number does for its zeros, but not an infinity or NaN, which page 0 may have:
+        // the call's own scale is one)
+        const float __attribute__((address_space(4))) *number = &rare()->scale;
+        const size_t scale_at = (size_t)id * Hkv + head;
+        k_sc = *(there ? (const float __attribute__((address_space(4))) *)(uintptr_t)k_scales + scale_at : number);
+        v_sc = *(there ? (const float __attribute__((address_space(4))) *)(uintptr_t)v_scales + scale_at : number);
         auto kb = __builtin_amdgcn_make_buffer_rsrc((void *)((const char *)k_pages + off), 0, bytes, 0x00020000);
         auto vb = __builtin_amdgcn_make_buffer_rsrc((void *)((const char *)v_pages + off), 0, bytes, 0x00020000);
         const int at_lane = lane_now() * (HD / 8);
