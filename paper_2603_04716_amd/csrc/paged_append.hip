@@ -175,10 +175,10 @@ __device__ __forceinline__ void recode(uint8_t *page, int slots, float ratio, in
 //
 // Which page a workgroup has follows from device data.  Sequence b touches at most rows / ps + 2 pages (rounded down), so
 // with first(b) = start(b) / ps + 2 b the workgroups first(b) .. first(b + 1) - 1 suffice for it, and a workgroup
-// finds its sequence by a search over starts alone.  Behind them the same launch has a workgroup for every few rows'
-// queries.
+// finds its sequence by a search over starts alone.  Behind them come workgroups for every few rows' queries.  `first` is the
+// launch's first workgroup of the call's.
 template <int HD, int NI>
-__global__ __launch_bounds__(256) void paged_append_codes_kernel(PagedAppendArgs a, int page_groups, int per_group)
+__global__ __launch_bounds__(256) void paged_append_codes_kernel(PagedAppendArgs a, int page_groups, int per_group, int first)
 {
     constexpr int HALF = HD / 2, TPR = HD / 16, RPR = 256 / TPR;   // threads of a row, rows of a round
     __shared__ float2 cs[kRowsPerGroup][HALF];
@@ -186,13 +186,13 @@ __global__ __launch_bounds__(256) void paged_append_codes_kernel(PagedAppendArgs
     __shared__ float red[2][4];
     const PagedView &p = a.p;
     const int tid = threadIdx.x;
-    const int pgs = page_groups * p.Hkv;
-    if ((int)blockIdx.x >= pgs) {
-        const int row0 = ((int)blockIdx.x - pgs) * per_group;
+    const int block = first + (int)blockIdx.x, pgs = page_groups * p.Hkv;
+    if (block >= pgs) {
+        const int row0 = (block - pgs) * per_group;
         append_rows<uint16_t, HD, false>(a, row0, min(per_group, p.n_rows - row0), cs, at);
         return;
     }
-    const int pj = blockIdx.x / p.Hkv, g = blockIdx.x - pj * p.Hkv;
+    const int pj = block / p.Hkv, g = block - pj * p.Hkv;
     const int ps_log = p.ps_log;
     const int b = wave_last_le(p.n_seqs, pj, [&](int i) { return (paged_start(p, i) >> ps_log) + 2 * i; });
     const int start = paged_start(p, b), rows = paged_rows(p, b, start), len = paged_len(p, b);
@@ -345,14 +345,23 @@ __global__ __launch_bounds__(256) void paged_append_one_kernel(PagedAppendArgs a
     *(uint2 *)(vp + off + HALF) = codes8(v[1], 1.f / v_new);
 }
 
+// Workgroups of a launch: 2^32 threads are more than a grid can have, and a call of 2^24 rows has up to 2^30 workgroups.
+constexpr int kAppendGroups = 1 << 23;
+
 template <int HD>
-static void launch_codes(const PagedAppendArgs &a, int page_groups, int per_group, unsigned grid, hipStream_t s)
+static hipError_t launch_codes(const PagedAppendArgs &a, int page_groups, int per_group, int groups, hipStream_t s)
 {
-    switch ((HD << a.p.ps_log) / 4096) {             // rounds that a full page takes
-    case 0: case 1: paged_append_codes_kernel<HD, 1><<<grid, 256, 0, s>>>(a, page_groups, per_group); break;
-    case 2: paged_append_codes_kernel<HD, 2><<<grid, 256, 0, s>>>(a, page_groups, per_group); break;
-    default: paged_append_codes_kernel<HD, 4><<<grid, 256, 0, s>>>(a, page_groups, per_group); break;
+    for (int first = 0; first < groups; first += kAppendGroups) {
+        const unsigned grid = (unsigned)(groups - first < kAppendGroups ? groups - first : kAppendGroups);
+        switch ((HD << a.p.ps_log) / 4096) {         // rounds that a full page takes
+        case 0: case 1: paged_append_codes_kernel<HD, 1><<<grid, 256, 0, s>>>(a, page_groups, per_group, first); break;
+        case 2: paged_append_codes_kernel<HD, 2><<<grid, 256, 0, s>>>(a, page_groups, per_group, first); break;
+        default: paged_append_codes_kernel<HD, 4><<<grid, 256, 0, s>>>(a, page_groups, per_group, first); break;
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
     }
+    return hipSuccess;
 }
 
 hipError_t launch_paged_append(int kind, int hd, const PagedAppendArgs &a, hipStream_t s)
@@ -367,9 +376,8 @@ hipError_t launch_paged_append(int kind, int hd, const PagedAppendArgs &a, hipSt
         else paged_append_one_kernel<64><<<grid, 256, 0, s>>>(a);
     } else if (kind == PAGED_E4M3) {
         const int page_groups = (a.p.n_rows >> a.p.ps_log) + 2 * a.p.n_seqs;
-        const unsigned grid = (unsigned)(page_groups * a.p.Hkv) + (a.q ? row_groups : 0u);
-        if (hd == 128) launch_codes<128>(a, page_groups, per_group, grid, s);
-        else launch_codes<64>(a, page_groups, per_group, grid, s);
+        const int groups = page_groups * a.p.Hkv + (a.q ? (int)row_groups : 0);
+        return hd == 128 ? launch_codes<128>(a, page_groups, per_group, groups, s) : launch_codes<64>(a, page_groups, per_group, groups, s);
     } else if (kind == PAGED_BF16) {
         if (hd == 128) paged_append_rows_kernel<uint16_t, 128><<<row_groups, 256, 0, s>>>(a, per_group);
         else paged_append_rows_kernel<uint16_t, 64><<<row_groups, 256, 0, s>>>(a, per_group);
