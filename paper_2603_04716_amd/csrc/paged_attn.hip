@@ -446,12 +446,19 @@ __global__ __launch_bounds__(256, KIND == PAGED_F32 ? 1 : 2) void paged_rows_ker
                 const float m_ref = m_new == -INFINITY ? 0.f : m_new;      // nothing seen yet: every weight is 0
                 const float alpha = pexp2(m_run[r] - m_ref);
                 m_run[r] = m_new;
-                float sum = 0.f;
+                float sum = 0.f, factor = sl2e;
+                if (__any(fabsf(m_ref) > kExactScores)) {
+                    factor = 1.f;
+#pragma unroll
+                    for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) s[r][kb][j] *= sl2e;
+                }
 #pragma unroll
                 for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        s[r][kb][j] = pexp2(fmaf(s[r][kb][j], sl2e, -m_ref));
+                        s[r][kb][j] = pexp2(fmaf(s[r][kb][j], factor, -m_ref));
                         sum += s[r][kb][j];
                     }
                 l_run[r] = l_run[r] * alpha + sum;

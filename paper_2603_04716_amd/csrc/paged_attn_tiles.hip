@@ -47,7 +47,7 @@ typedef s16x4 __attribute__((address_space(3))) *trptr_t;
 #define PD_TILE_LGKM0() __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14))
 
 constexpr int kTileRows = 256, kTileKeys = 64;
-constexpr float kNoScore = -3.0e38f;             // running maximum before any score: finite, so that differences are defined
+constexpr float kNoScore = -0x1.fffffep127f;      // running maximum before any score: the least finite number, so that differences are defined
 constexpr float kLazyRaise = 8.0f;               // the maximum is raised when a score exceeds it by 2^8: sums stay exact in fp32
 
 // Byte offset of the 16-byte piece c of row r in a K or V tile.  K is read 32 rows at one piece index, V four rows at 64
@@ -129,6 +129,7 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
     bf16x8 qf[NK];                                   // 0 .. w_min - 1, the lane's row 0 .. limit - 1
     f32x16 o[NDB];
     float m_run, l_run;
+    bool large;                                      // some row's maximum is beyond kExactScores
     // A unit's row w is (token, head) row r0 + w of its sequence: token tok + (rest + w) / G, where G tok + rest = r0.  The quotient by
     // way of fp32 is exact for dividends up to 2^21.
     struct Unit {
@@ -184,6 +185,7 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
         limit = x.limit;
         m_run = kNoScore;
         l_run = 0.f;
+        large = false;
 #pragma unroll
         for (int i = 0; i < NDB; ++i)
 #pragma unroll
@@ -397,18 +399,26 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
         if (__any(m_cand - m_run > kLazyRaise)) {
             const float alpha = pexp2(m_run - m_cand);
             m_run = m_cand;
+            large |= __any(fabsf(m_cand) > kExactScores && m_cand != kNoScore);
             l_run *= alpha;
 #pragma unroll
             for (int i = 0; i < NDB; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[i][r] *= alpha;
         }
-        float sum = 0.f;
+        float sum = 0.f, factor = sl2e;
+        if (large) {
+            factor = 1.f;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[kb][r] *= sl2e;
+        }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[kb][r] = pexp2(fmaf(s[kb][r], sl2e, -m_run));
+                s[kb][r] = pexp2(fmaf(s[kb][r], factor, -m_run));
                 sum += s[kb][r];
             }
         l_run += sum;

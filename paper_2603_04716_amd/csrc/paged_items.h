@@ -15,6 +15,11 @@ namespace pd {
 
 __device__ __forceinline__ float pexp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// 2^(score * scale - m) by a fused product: what rounding leaves of m = rounded(largest * scale), up to half a step of m, is in
+// all weights of a row alike, and harmless while it is small.  From here on the products are rounded as m is, so that the largest
+// weight is 1 however large the scores are.
+constexpr float kExactScores = 0x1p24f;
+
 // Sum over the lanes up to this one, by data-parallel moves: a cross-lane step through LDS would take ten times as long, and every
 // workgroup waits for the division before its first load.
 template <typename T>

@@ -37,3 +37,31 @@ def test_missing_pages_are_zeros_whatever_the_scales_of_a_page_of_nobody(hd, num
         got = c.attend()
         c.ks[0], c.vs[0] = 1.0, 1.0                              # (the oracle's zeros take no scale; its arrays have to be numbers)
         check(c, got)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "e4m3"])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("q_log,k_log,scale", [(2, 3, 0.3), (20, 13, 0.3), (20, 13, 0.7), (60, 40, 0.3), (67, 60, float(np.float32(np.log(2.0))))])
+def test_scores_of_any_size(kind, sign, q_log, k_log, scale):
+    """Scores of up to 3.2e38 (the softmax in base 2): equal ones share a row's weight, and a larger one has all of it.  One channel
+    makes the score, so that it is one exact product, the same for all keys but one."""
+    # rows of both kernels, contexts that are split, and single rows
+    for seqs, starts in (([(1, 40), (3, 700), (100, 130), (150, 6000), (2, 9000), (5, 2)], True), ([(1, 300), (1, 9000), (1, 1)], False)):
+        c = Paged(kind, 4, 2, 64, 32, seqs, seed=q_log, starts=starts)
+        q = torch.zeros_like(c.q)
+        q[:, :, 0] = sign * 2.0 ** q_log
+        some, one = (1.875, 0.9375) if sign < 0 else (0.9375, 1.875)
+        if kind == "e4m3":
+            c.ks.fill_(2.0 ** k_log)
+        else:
+            some, one = some * 2.0 ** k_log, one * 2.0 ** k_log
+        c.k[:, :, :, 0] = torch.tensor(some).to(c.k.dtype).cuda()
+        for b, n in enumerate(c.lens_h):
+            if b % 2 and n > 2:
+                c.k[int(c.table_h[b, (n - 2) // 32]), :, (n - 2) % 32, 0] = torch.tensor(one).to(c.k.dtype).cuda()
+        got = c.attend(q=q, scale=scale)
+        want, weight, delta = P.attend(*c.host(), c.starts_h, c.lens_h, c.table_h, f64(q), scale)
+        if q_log > 2:
+            delta[:] = 0.0                                       # the scores are exact but for one rounding that all share
+        bound = attention_bound(kind, want, weight, delta, c.lens_h, c.starts_h, 64)
+        assert (np.abs(f64(got) - want) <= bound).all()
