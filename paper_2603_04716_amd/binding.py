@@ -331,7 +331,6 @@ def make_paged_kv(k_pages, v_pages, k_scales=None, v_scales=None):
     kv = pd_paged_kv(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr() if codes else None, v_scales.data_ptr() if codes else None,
                      n, ps, h, hd, PD_F32 if k_pages.dtype == torch.float32 else PD_BF16, int(codes))
     kv.tensors, kv.device = (k_pages, v_pages, k_scales, v_scales), devices.pop()
-    kv.row_type, kv.heads, kv.hd = torch.float32 if k_pages.dtype == torch.float32 else torch.bfloat16, h, hd      # (for the checks of a call)
     return kv
 
 
@@ -349,7 +348,7 @@ def make_paged_seqs(lens, page_table, row_starts=None, n_rows=None):
         raise ValueError("make_paged_seqs: page_table [n_seqs, table_width], row_starts [n_seqs + 1] together with n_rows")
     seqs = pd_paged_seqs(n, n if n_rows is None else int(n_rows), None if row_starts is None else row_starts.data_ptr(), lens.data_ptr(),
                          page_table.data_ptr(), page_table.shape[1])
-    seqs.tensors, seqs.device, seqs.rows = (lens, page_table, row_starts), devices.pop(), seqs.n_rows
+    seqs.tensors, seqs.device = (lens, page_table, row_starts), devices.pop()
     return seqs
 
 
@@ -365,10 +364,9 @@ def _paged_stream(who, kv, seqs, tensors):
     return stream.cuda_stream
 
 
-def _paged_stride(who, t, kv, rows, heads):
+def _paged_stride(who, t, row_type, rows, heads, hd):
     """Row stride of t [n_rows, heads, head_dim] whose rows hold their heads next to each other."""
-    hd = kv.hd
-    if t.dtype is not kv.row_type or t.shape != (rows, heads, hd):
+    if t.dtype is not row_type or t.shape != (rows, heads, hd):
         raise ValueError(f"{who}: tensors are [n_rows, heads, head_dim] in the cache's row type")
     row, head, one = t.stride()
     if (one != 1 or (heads > 1 and head != hd)) and rows > 0:
@@ -376,10 +374,16 @@ def _paged_stride(who, t, kv, rows, heads):
     return row if rows > 1 else heads * hd
 
 
+def _paged_sizes(kv, seqs):
+    """What the tensors of a call have to be: row type, rows and head_dim, as the descriptors say now (a caller may set n_rows)."""
+    return torch.float32 if kv.dtype == PD_F32 else torch.bfloat16, seqs.n_rows, kv.head_dim
+
+
 def pd_paged_append(kv, seqs, k, v, rope_base=0.0, q=None, q_out=None):
     """k, v [n_rows, n_kv_heads, head_dim] into the pages of kv; q [n_rows, n_q_heads, head_dim] rotated into q_out."""
-    who, n, h = "pd_paged_append", seqs.rows, kv.heads
-    strides = _paged_stride(who, k, kv, n, h), _paged_stride(who, v, kv, n, h)
+    who, h = "pd_paged_append", kv.n_kv_heads
+    row_type, n, hd = _paged_sizes(kv, seqs)
+    strides = _paged_stride(who, k, row_type, n, h, hd), _paged_stride(who, v, row_type, n, h, hd)
     if q is None:
         if q_out is not None:
             raise ValueError(f"{who}: q and q_out belong together")
@@ -389,8 +393,8 @@ def pd_paged_append(kv, seqs, k, v, rope_base=0.0, q=None, q_out=None):
         if q_out is None or q.dim() != 3:
             raise ValueError(f"{who}: q [n_rows, n_q_heads, head_dim] and q_out belong together")
         hq = q.shape[1]
-        rows = pd_paged_rows(k.data_ptr(), v.data_ptr(), q.data_ptr(), q_out.data_ptr(), *strides, _paged_stride(who, q, kv, n, hq),
-                             _paged_stride(who, q_out, kv, n, hq), hq, rope_base)
+        rows = pd_paged_rows(k.data_ptr(), v.data_ptr(), q.data_ptr(), q_out.data_ptr(), *strides, _paged_stride(who, q, row_type, n, hq, hd),
+                             _paged_stride(who, q_out, row_type, n, hq, hd), hq, rope_base)
         stream = _paged_stream(who, kv, seqs, (k, v, q, q_out))
     _check(lib.pd_paged_append(C.byref(kv), C.byref(seqs), C.byref(rows), stream))
 
@@ -407,11 +411,12 @@ def pd_paged_attention(kv, seqs, q, out, workspace, scale=None):
     who = "pd_paged_attention"
     if q.dim() != 3:
         raise ValueError(f"{who}: q is [n_rows, n_q_heads, head_dim]")
-    stride = _paged_stride(who, q, kv, seqs.rows, q.shape[1])
+    row_type, n, hd = _paged_sizes(kv, seqs)
+    stride = _paged_stride(who, q, row_type, n, q.shape[1], hd)
     if out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous() or not workspace.is_contiguous():
         raise ValueError(f"{who}: out is a contiguous tensor like q, the workspace a contiguous tensor")
     _check(lib.pd_paged_attention(C.byref(kv), C.byref(seqs), q.data_ptr(), stride, q.shape[1],
-                                  kv.head_dim ** -0.5 if scale is None else scale, out.data_ptr(),
+                                  hd ** -0.5 if scale is None else scale, out.data_ptr(),
                                   workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                   _paged_stream(who, kv, seqs, (q, out, workspace))))
     return out

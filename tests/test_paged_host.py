@@ -157,3 +157,22 @@ def test_descriptors_refuse_other_tensors():
             pd.pd_paged_append(kv, seqs, bad, rows[:, 2:4])
     with pytest.raises(ValueError):
         pd.pd_paged_attention(kv, seqs, rows[:, :4].contiguous(), rows[:, :4], rows)
+
+
+def test_sizes_set_in_a_descriptor_are_the_sizes_that_tensors_are_held_to():
+    """A program that sets a descriptor's n_rows for its next call may not have a kernel read rows that its tensors do not have."""
+    kv = pd.make_paged_kv(torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16), torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16))
+    seqs = pd.make_paged_seqs(torch.zeros(3, dtype=torch.int32), torch.zeros(3, 5, dtype=torch.int32), torch.zeros(4, dtype=torch.int32), 7)
+    rows = torch.zeros(7, 4, 64, dtype=torch.bfloat16)
+    seqs.n_rows = 9
+    with pytest.raises(ValueError):
+        pd.pd_paged_append(kv, seqs, rows[:, :2], rows[:, 2:])
+    with pytest.raises(ValueError):
+        pd.pd_paged_attention(kv, seqs, rows, torch.zeros_like(rows), rows)
+    seqs.n_rows = 7
+    kv.n_kv_heads = 3
+    with pytest.raises(ValueError):
+        pd.pd_paged_append(kv, seqs, rows[:, :2], rows[:, 2:])
+    kv.n_kv_heads, kv.head_dim = 2, 128
+    with pytest.raises(ValueError):
+        pd.pd_paged_attention(kv, seqs, rows, torch.zeros_like(rows), rows)
