@@ -65,3 +65,52 @@ def test_scores_of_any_size(kind, sign, q_log, k_log, scale):
             delta[:] = 0.0                                       # the scores are exact but for one rounding that all share
         bound = attention_bound(kind, want, weight, delta, c.lens_h, c.starts_h, 64)
         assert (np.abs(f64(got) - want) <= bound).all()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_key_codes_that_are_not_numbers(hd):
+    """A NaN code among a sequence's keys: the rows that see it are NaN in the heads that read it, no other element changes."""
+    c = Paged("e4m3", 4, 2, hd, 32, [(100, 130), (3, 700), (1, 90), (60, 5000), (40, 40)], seed=32)
+    clean = c.attend()
+    check(c, clean)
+    x = c.k.view(torch.uint8)
+    hit = torch.zeros_like(clean, dtype=torch.bool)
+    for b, p, g, code in ((0, 70, 0, 0x7F), (1, 650, 1, 0xFF), (2, 0, 0, 0x7F), (3, 1234, 1, 0xFF), (4, 39, 0, 0x7F)):
+        x[int(c.table_h[b, p // 32]), g, p % 32, 5] = code
+        first = int(c.starts_h[b]) + max(p - (c.lens_h[b] - c.new[b]), 0)
+        hit[first:int(c.starts_h[b + 1]), 2 * g:2 * g + 2] = True
+    got = c.attend()
+    assert torch.isnan(got[hit]).all() and torch.equal(got[~hit], clean[~hit])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_infinite_keys_in_chunks_and_prompts(kind):
+    """Scores of -infinity weigh nothing, rows that see no other score are 0 / 0, a score of infinity makes the rows that see it NaN: in
+    chunks whose rows see different keys, and in a context that is split."""
+    c = Paged(kind, 4, 2, 64, 16, [(100, 100), (70, 400), (40, 6000), (3, 60)], seed=33)
+    q = c.q.clone()
+    q[:, :, 0] = 1.0
+    for b, keys in ((0, [0, 1, 2, 50, 99]), (1, list(range(0, 400, 7))), (2, list(range(0, 2000))), (3, [0, 59])):
+        for p in keys:
+            c.k[int(c.table_h[b, p // 16]), :, p % 16, 0] = float("-inf")
+    scale = 64 ** -0.5
+
+    def held_to(got):
+        with np.errstate(invalid="ignore"):
+            want, weight, _ = P.attend(*c.host(), c.starts_h, c.lens_h, c.table_h, f64(q), scale)
+        k = c.k.clone()
+        k[..., 0] = torch.where(torch.isfinite(k[..., 0]), k[..., 0], 0.0)
+        _, _, delta = P.attend(f64(k), f64(c.v), None, None, c.starts_h, c.lens_h, c.table_h, f64(q), scale)
+        g, nan = f64(got), np.isnan(want)
+        assert (np.isnan(g) == nan).all()
+        bound = attention_bound(kind, want, weight, delta, c.lens_h, c.starts_h, 64)
+        assert (np.abs(g - want)[~nan] <= bound[~nan]).all()
+        return nan
+
+    nan = held_to(c.attend(q=q))
+    assert nan[:3].all() and not nan[3:].any()
+    for b, p in ((0, 60), (1, 350), (2, 5990)):
+        c.k[int(c.table_h[b, p // 16]), :, p % 16, 0] = float("inf")
+    nan = held_to(c.attend(q=q))
+    # (rows 170 .. 209 are positions 5960 .. 5999 of the third sequence)
+    assert nan[60:100].all() and not nan[3:60].any() and not nan[170:200].any() and nan[200:210].all() and not nan[210:].any()
