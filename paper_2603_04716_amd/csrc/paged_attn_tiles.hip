@@ -466,7 +466,7 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
     };
     // A weight of 0 times a value that is infinite or NaN is NaN: such a value would reach rows that do not see it.  The results
     // tell: where one is not finite, the tiles are gone through again with the values in question taken out in LDS, and these
-    // are then added to the rows that see them.
+    // are then looked for in the pages and added to the rows that see them.
     bool clean = false;
     auto clean_v = [&](unsigned char *st) __attribute__((always_inline)) {    // by the early half of the waves in M(j), before any S(j)
         if (!late)
@@ -507,21 +507,49 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
             const auto args = rare();
             const int g = PD_ITEM(item, g);
             const int32_t *table = args->p.table + (size_t)PD_ITEM(item, seq) * args->p.width;
-            const int end = min(t_hi * kTileKeys, PD_ITEM(item, seen));
+            const int last = min(t_hi * kTileKeys, PD_ITEM(item, seen));
+            const int32_t pages_end = args->p.n_pages, log = args->p.ps_log;
+            constexpr int E = KIND == PAGED_E4M3 ? 1 : 2, STEP = 16;     // keys that share a page at every page size
+            auto rows_at = [&](int id, int key) __attribute__((always_inline)) {
+                return (((size_t)id * args->p.Hkv + g) << log) + (key & ((1 << log) - 1));
+            };
 #pragma unroll 1
-            for (int key = PD_ITEM(item, t_lo) * kTileKeys; key < end; ++key) {
-                const int id = load_const(table, key >> args->p.ps_log);
-                if (id < 0 || id >= args->p.n_pages) continue;
-                const size_t unit = (size_t)id * args->p.Hkv + g, at_v = ((unit << args->p.ps_log) + (key & ((1 << args->p.ps_log) - 1))) * HD;
-                const float v_scale = KIND == PAGED_E4M3 ? load_const(args->p.v_scales, unit) : 1.f;
+            for (int tile = PD_ITEM(item, t_lo); tile < t_hi; ++tile) {
+                unsigned found = 0;                  // steps of the tile with such values (or, in unused slots, numbers that look like one)
 #pragma unroll
-                for (int db = 0; db < NDB; ++db)
+                for (int i = 0; i < kTileKeys / STEP; ++i) {
+                    const int key = tile * kTileKeys + STEP * i, id = key < last ? load_const(table, key >> log) : -1;
+                    if (id < 0 || id >= pages_end) continue;
+                    const u32x4 *rows = (const u32x4 *)((const char *)args->p.v + rows_at(id, key) * (HD * E));
+                    unsigned odd = KIND == PAGED_E4M3 && !(load_const(args->p.v_scales, (size_t)id * args->p.Hkv + g) < 0x1p120f);    // (256 * 2^120 is infinite)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const size_t i = at_v + 32 * db + 8 * (r >> 2) + 4 * h + (r & 3);
-                        const float x = KIND == PAGED_E4M3 ? e4m3_decode(((const uint8_t *)args->p.v)[i]) * v_scale : bfbits2f(((const uint16_t *)args->p.v)[i]);
-                        if (!(fabsf(x) < INFINITY) && key < limit) o[db][r] += x;
+                    for (int k = 0; k < STEP * HD * E / 1024; ++k) {
+                        const u32x4 w = rows[64 * k + lane];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if (KIND == PAGED_E4M3) odd |= ((w[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;       // a byte of 0x7f or 0xff
+                            else odd |= (((w[e] & 0x7f807f80u) >> 7) + 0x00010001u) & 0x01000100u;                    // an exponent of ones
+                        }
                     }
+                    if (__any(odd != 0)) found |= 1u << i;
+                }
+                for (; found; found &= found - 1) {
+                    const int first = tile * kTileKeys + STEP * (__ffs(found) - 1);
+                    const int id = load_const(table, first >> log);
+                    const float v_scale = KIND == PAGED_E4M3 ? load_const(args->p.v_scales, (size_t)id * args->p.Hkv + g) : 1.f;
+#pragma unroll 1
+                    for (int key = first; key < min(first + STEP, last); ++key) {
+                        const size_t at_v = rows_at(id, key) * HD;
+#pragma unroll
+                        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) {
+                                const size_t i = at_v + 32 * db + 8 * (r >> 2) + 4 * h + (r & 3);
+                                const float x = KIND == PAGED_E4M3 ? e4m3_decode(((const uint8_t *)args->p.v)[i]) * v_scale : bfbits2f(((const uint16_t *)args->p.v)[i]);
+                                if (!(fabsf(x) < INFINITY) && key < limit) o[db][r] += x;
+                            }
+                    }
+                }
             }
         }
         const float l_tot = l_run + __shfl_xor(l_run, 32, 64);

@@ -114,3 +114,33 @@ def test_infinite_keys_in_chunks_and_prompts(kind):
     nan = held_to(c.attend(q=q))
     # (rows 170 .. 209 are positions 5960 .. 5999 of the third sequence)
     assert nan[60:100].all() and not nan[3:60].any() and not nan[170:200].any() and nan[200:210].all() and not nan[210:].any()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_values_that_are_not_finite_in_long_parts(kind):
+    """Parts of more than 512 tiles of keys, sequences that read the same pages: infinities and NaN in a few of the tiles reach the
+    rows that see them, in their channels, and nothing else; a NaN in a query or a key reaches the rows that it makes."""
+    hkv, new, length = 32, 40, 45000
+    c = Paged(kind, 8 * hkv, hkv, 64, 128, [(new, length)] + [(new, 1)] * 7, seed=34, extra_width=0)
+    c.table_h[:] = c.table_h[0]
+    c.lens_h = [length] * 8
+    c.bind()
+    clean = c.attend()
+    assert torch.isfinite(clean).all()
+    x, odd = (c.v.view(torch.uint8), 0x7F) if kind == "e4m3" else (c.v, float("nan"))
+    hit = torch.zeros_like(clean, dtype=torch.bool)
+    for p, g, ch in ((0, 0, 5), (63, 0, 6), (64, 3, 7), (20000, 3, 8), (33000, 31, 63), (length - new - 1, 30, 0), (length - 7, 30, 1), (length - 1, 30, 2)):
+        x[int(c.table_h[0, p // 128]), g, p % 128, ch] = odd
+        for b in range(8):
+            hit[b * new + max(p - (length - new), 0):(b + 1) * new, 8 * g:8 * g + 8, ch] = True
+    got = c.attend()
+    assert torch.isnan(got[hit]).all() and torch.equal(got[~hit], clean[~hit])
+    q = c.q.clone()
+    q[77, 100, 3] = float("nan")
+    hit[77, 100] = True
+    got = c.attend(q=q)
+    assert torch.isnan(got[hit]).all() and torch.equal(got[~hit], clean[~hit])
+    (c.k.view(torch.uint8) if kind == "e4m3" else c.k)[int(c.table_h[0, 100]), 7, 3, 9] = odd
+    hit[:, 56:64] = True
+    got = c.attend(q=q)
+    assert torch.isnan(got[hit]).all() and torch.equal(got[~hit], clean[~hit])
