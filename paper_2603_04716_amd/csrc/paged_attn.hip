@@ -216,19 +216,21 @@ struct Step<PAGED_E4M3, HD> : Step16<Step<PAGED_E4M3, HD>, HD> {
 #pragma unroll
         for (int d = 0; d < CPL / 4; ++d) v[i][d] = 0u;
     }
-    __device__ __forceinline__ bool take_odd()       // the codes 0x7f and 0xff are not numbers; there are no infinities
+    __device__ __forceinline__ bool take_odd()       // the codes 0x7f and 0xff are not numbers, and 256 * 2^120 is infinite
     {
         bool odd = false;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 8; ++i) {
+            const unsigned least = vs[i >> 2] < 0x1p120f ? 0x7fu : 0x78u;
 #pragma unroll
             for (int d = 0; d < CPL / 4; ++d)
 #pragma unroll
                 for (int e = 0; e < 32; e += 8)
-                    if ((v[i][d] >> e & 0x7fu) == 0x7fu) {
+                    if ((v[i][d] >> e & 0x7fu) >= least) {
                         v[i][d] &= ~(0xffu << e);
                         odd = true;
                     }
+        }
         return odd;
     }
     static __device__ __forceinline__ float value(elem x, float scale) { return e4m3_decode(x) * scale; }

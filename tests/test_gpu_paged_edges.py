@@ -144,3 +144,24 @@ def test_values_that_are_not_finite_in_long_parts(kind):
     hit[:, 56:64] = True
     got = c.attend(q=q)
     assert torch.isnan(got[hit]).all() and torch.equal(got[~hit], clean[~hit])
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_values_of_the_largest_scale(hd):
+    """At a scale of 2^120 the codes of 256 and more are infinite: rows behind them are that, rows before them as without."""
+    for seqs, starts, at in (([(3, 40), (100, 130), (40, 9000)], True, (38, 118, 8980)), ([(1, 40), (1, 5000)], False, (38, 4000))):
+        c = Paged("e4m3", 2, 1, hd, 16, seqs, seed=35, starts=starts)
+        for b, p in enumerate(at):
+            page = int(c.table_h[b, p // 16])
+            c.v.view(torch.uint8)[page] = 0
+            c.vs[page] = 2.0 ** 120
+        clean = c.attend()
+        check(c, clean)
+        for code, value in ((0x7E, float("inf")), (0xF8, float("-inf")), (0x7F, float("nan"))):
+            hit = torch.zeros_like(clean, dtype=torch.bool)
+            for b, p in enumerate(at):
+                c.v.view(torch.uint8)[int(c.table_h[b, p // 16]), 0, p % 16, 5] = code
+                hit[int(c.starts_h[b]) + max(p - (c.lens_h[b] - c.new[b]), 0):int(c.starts_h[b + 1]), :, 5] = True
+            got = c.attend()
+            assert torch.equal(got[~hit], clean[~hit])
+            assert torch.isnan(got[hit]).all() if value != value else (got[hit] == value).all()
