@@ -211,3 +211,21 @@ def test_pool_of_more_than_4_gib():
     pd.pd_paged_attention(kv, seqs, rows[:, :hkv], out, ws)
     # the first row sees itself alone: its value, as the page holds it
     torch.testing.assert_close(out[0].float(), (got * scale)[0].to(torch.bfloat16).float(), rtol=0, atol=0)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("starts", [True, False])
+def test_full_pages_whose_scales_grow(hd, starts):
+    """One row in the last slots of pages, whose scales are too small by up to 2^20: every older code is rounded again."""
+    for ps in (16, 64, 128):
+        lens = [ps, ps - 1, 2 * ps, 3 * ps - 1, ps // 2 + 1, 2]
+        c = Paged("e4m3", 2, 2, hd, ps, [(1, n) for n in lens], seed=ps + hd, starts=starts)
+        rng = np.random.default_rng(ps + hd)
+        for s in (c.ks, c.vs):
+            s *= torch.from_numpy(2.0 ** -rng.integers(0, 21, tuple(s.shape))).float().cuda()
+        c.bind()
+        before = c.host()
+        q, k, v = c.parts()
+        q_out = torch.full((c.n_rows, 2, hd), 7.0, dtype=q.dtype, device="cuda")
+        pd.pd_paged_append(c.kv, c.seqs, k, v, BASE, q, q_out)
+        check(c, before, BASE, True, q_out)
