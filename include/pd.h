@@ -212,7 +212,9 @@ pd_status pd_kv_cache_get(const pd_kv_cache *cache, int32_t slot, int32_t len, v
  *   k, v          device [n_pages, n_kv_heads, page_size, head_dim], 16-byte aligned, elements of dtype or, with e4m3 set,
  *                 OCP E4M3 codes
  *   k_scales, v_scales   device fp32 [n_pages, n_kv_heads], e4m3 only: an element is scale * value(code).  A scale is a
- *                 power of two between 2^-60 and 2^120, as pd_paged_append makes them
+ *                 power of two between 2^-60 and 2^120, as pd_paged_append makes them (at 2^120 codes of 256 and more are infinite:
+ *                 a bf16 value from 1.9375 * 2^127 on is rounded to one).  Scales of pages that hold no position of the call's
+ *                 sequences may be anything
  *   page_size     16, 32, 64 or 128;  head_dim 64 or 128;  dtype the type of the rows (e4m3: PD_BF16)
  */
 typedef struct {
@@ -268,7 +270,8 @@ typedef struct {
  * slot 0 and max(old scale, s(A)) otherwise; codes of the page's earlier positions are then rounded again to the larger
  * scale (exact except for what becomes subnormal).  New elements are coded as by pd_quantize_rows_e4m3: nearest, ties to
  * even, saturating at +-448; NaN stays NaN.  Slots behind the sequence's last position are left as they were.
- * A page that receives rows belongs to one sequence of the call: two sequences may share pages that they only read.
+ * A page that receives rows belongs to one sequence of the call and stands once among its pages: two sequences may share pages
+ * that they only read.
  * Asynchronous on stream.  Errors: PD_ERR_INVALID_ARG (NULL, misaligned pointers, counts or rope_base out of range),
  * PD_ERR_SHAPE (sizes, strides), PD_ERR_DTYPE, PD_ERR_DEVICE.
  */
@@ -281,7 +284,9 @@ pd_status pd_paged_append(const pd_paged_kv *kv, const pd_paged_seqs *seqs, cons
  * step, several are drafted tokens or a chunk, lens equal to the rows a whole prompt, in any mixture.
  * q [n_rows, n_q_heads, head_dim] with a row stride in elements as above; out [n_rows, n_q_heads, head_dim] contiguous, 16-byte
  * aligned; it does not overlap q or the pages.  Scores, softmax and sums in fp32; in bf16 the exponentials are rounded to bf16 before they weigh the values.
- * Results do not depend on what else is in a page: unused slots, later positions and infinities or NaN in them.
+ * Results do not depend on what else is in a page: unused slots, later positions and infinities or NaN in them.  Such values cost
+ * time where more than 32 (row, head) pairs of a sequence share a kv head: tiles of 256 pairs one of whose results is not finite
+ * are gone through a second time.
  * A row without a visible position gets zeros.
  * workspace: device memory, 16-byte aligned, of at least pd_paged_attention_workspace bytes for the same host-side sizes
  * (n_rows, n_seqs, table_width, whether row_starts is NULL); it needs no initial value, holds nothing between calls, and is not

@@ -3,9 +3,9 @@
 //   y[c] = x[c] cos - x[c + hd/2] sin,  y[c + hd/2] = x[c] sin + x[c + hd/2] cos,  angle = position * base^(-2c / hd)
 //
 // Nothing is used twice, so the floor is the rows read once and the pages and rotated queries written once.  The angle is
-// formed in double as turns (position * base^(-2c/hd) / 2 pi) and reduced to half a turn before it becomes fp32: that is
-// exact to 1e-7 at every position that an int32 holds, at three double-precision instructions instead of a
-// double-precision sine.  Measured, heads of 128: 24 chunks of up to 700 rows, 40 heads on 8, bf16, 57 us or 4.3 TB/s (a large copy
+// formed in double as turns (position * base^(-2c/hd) / 2 pi) and reduced to half a turn before it becomes fp32, at three
+// double-precision instructions instead of a double-precision sine: the rest is within 3e-9 rad at positions up to 2^24 and 2e-7
+// rad at 2^30, and fp32 rounds it by 9e-8.  Measured, heads of 128: 24 chunks of up to 700 rows, 40 heads on 8, bf16, 57 us or 4.3 TB/s (a large copy
 // reaches 4.9); four prompts of 2048, 32 heads on 8, to E4M3 pages 47 us or 4.0 TB/s; one row 3.4 us, which is a launch.
 #include "paged.h"
 
@@ -274,7 +274,9 @@ __global__ __launch_bounds__(256) void paged_append_codes_kernel(PagedAppendArgs
 }
 
 // E4M3 pages, one row per sequence: HD / 16 lanes have a head of a row - a query head, or a kv head's key and value - and with it
-// all that the call brings to its page, so that nothing has to be exchanged beyond those lanes.  256 sequences: 5.9 us.
+// all that the call brings to its page, so that nothing has to be exchanged beyond those lanes.  256 sequences: 5.8 us where no scale
+// grows.  Where one does, its lanes recode the page slot by slot, keys before values, and the launch takes as long as the fullest of
+// such pages: 21 us with 15 slots, 64 with up to 63, 127 with 127.
 template <int HD>
 __global__ __launch_bounds__(256) void paged_append_one_kernel(PagedAppendArgs a)
 {

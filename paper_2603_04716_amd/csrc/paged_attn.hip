@@ -17,8 +17,8 @@
 // (v_perm_b32, one per register), which takes no LDS and no lane crossing; accumulator c of a lane is then channel
 // (hd / 16) m + c of the matrix row m, 32 (hd 128) neighbouring channels per lane in all.
 //
-// Measured, 32 heads on 8 of 128 channels, one row per sequence: 64 sequences of 100 to 8000 positions 170 us or 5.7 TB/s, one of 131000
-// 92 us or 5.8 TB/s, 256 of 1500 to 2600 on E4M3 pages 192 us or 5.5 TB/s, and 5 us each for the partials.
+// Measured, 32 heads on 8 of 128 channels, one row per sequence: 64 sequences of 100 to 8000 positions 175 us or 5.6 TB/s, one of 131000
+// 94 us or 5.7 TB/s, 256 of 1500 to 2600 on E4M3 pages 193 us or 5.5 TB/s (a stream of reads reaches 6.2), and 5 us each for the partials.
 #include <string.h>
 
 #include <algorithm>
@@ -99,6 +99,9 @@ struct Step16 {                                      // bf16 operands, 32 keys: 
             r[j] = __builtin_amdgcn_perm(me.pair(2 * j + 1, c >> 1), me.pair(2 * j, c >> 1), c & 1 ? 0x07060302u : 0x05040100u);
         return r;
     }
+    // The exponentials are rounded to bf16, to be an operand of the matrix pipe (in fp32 the second product would take eight times
+    // as long): each weight by up to 2^-8 of itself, so that a result is off by at most that share of sum p |v| / sum p, and mostly by
+    // much less, as the roundings are of both signs.  The sum below the fraction adds them unrounded.
     static __device__ __forceinline__ bf16x8 operand(const f32x4 (&p)[NKB])
     {
         return __builtin_bit_cast(bf16x8, u32x4{pack2bf(p[0][0], p[0][1]), pack2bf(p[0][2], p[0][3]), pack2bf(p[1][0], p[1][1]), pack2bf(p[1][2], p[1][3])});
@@ -685,8 +688,8 @@ constexpr int kFewRows = 32;        // (token, head) rows of a sequence and kv h
 // Its workgroups: two on each of the 256 CUs.  64 sequences of 2000 positions take 97 us so, 100 us with half as many, and 100 us with
 // twice as many, whose partials are twice as many too (32 sequences of 4 rows: 66, 61 and 73 us).
 constexpr int kStreams = 512;
-// Most blocks that a table has room for up to which no unit is split, which saves the partials and the kernel that adds them up;
-// for fewer than 32 units, which leave most CUs idle, and for more.  8 kv heads, bf16, one sequence of 700 positions: 12.1 us so and
+// Most blocks that a table has room for (the host knows no lengths: a wide table is planned for long ones) up to which no unit is
+// split, which saves the partials and the kernel that adds them up; for fewer than 32 units, which leave most CUs idle, and for more.  8 kv heads, bf16, one sequence of 700 positions: 12.1 us so and
 // 12.9 us split, of 1000: 14.6 and 12.3 us; 64 sequences of up to 1000: 41 and 51 us, 256: 154 and 152 us.  (fp32, nine chunks of up to
 // 60 rows at up to 960 positions, 15 blocks: 25 and 16 us.)
 constexpr int kWholeBlocksFew = 6, kWholeBlocks = 8;

@@ -21,8 +21,8 @@
 // from unit to unit with the ring full, which saves the division of the call, the first loads' latency and an empty pipe, some
 // 13 us, for each unit but its first.
 //
-// Measured, 32 heads on 8 of 128 channels: four prompts of 2048 tokens in 166 us, 830 TFLOP/s of what the rows see (a square library
-// product of 8192 reaches 1232 here); 512 tokens behind 32000 in 291 us, 930 TFLOP/s.  A tile takes some 4000 clocks, of which the
+// Measured, 32 heads on 8 of 128 channels: calls of four prompts of 2048 tokens in 163 us, 840 TFLOP/s of what the rows see (large library
+// products reach 1230 to 1500 here, by their data); 512 tokens behind 32000 in 276 us, 980 TFLOP/s.  A tile takes some 4000 clocks, of which the
 // matrix pipe is busy for 2048: M, the two products, takes 1750 and S, the softmax, 1600 beside it, with 130 for a barrier each.
 // From unit to unit takes 4.5 us, from the launch to the first products 12 us.  Four waves of 64 rows, which read every operand half as
 // often but leave a SIMD one wave, took 5300 clocks a tile.
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(512, 1) void paged_tiles_kernel(PagedAttnArgs a)
         l_run += sum;
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
-            const int r = 8 * (ks & 1);
+            const int r = 8 * (ks & 1);              // (rounded to bf16 for the matrix pipe: 2^-8 of each weight at most, see Step16::operand)
             u32x4 w = {pack2bf(s[ks >> 1][r], s[ks >> 1][r + 1]), pack2bf(s[ks >> 1][r + 2], s[ks >> 1][r + 3]),
                        pack2bf(s[ks >> 1][r + 4], s[ks >> 1][r + 5]), pack2bf(s[ks >> 1][r + 6], s[ks >> 1][r + 7])};
             asm volatile("" : "+v"(w));              // formed in this phase, not where it is used

@@ -7,8 +7,8 @@
 // ahead of a unit has a closed form, and where the parts hold whole pairs, as those of equal prompts mostly do, nothing is split.
 // A border closer than `margin` to an end of its unit moves there: a partial of few tiles costs more than the
 // unevenness.  Every workgroup finds the same cut for a border, and as tiles count less than `per` each, cuts inside a unit are
-// different tiles.  Of kUnitKeys 192, 256 and 384 a call of twelve chunks of 1 to 700 tokens behind up to 6000 takes 308, 295 and 299 us,
-// with margins of an eighth, a 16th and a 32nd of a part 311, 292 and 295 us.
+// different tiles.  Of kUnitKeys 192, 256 and 384 a call of twelve chunks of 1 to 700 tokens behind up to 6000 takes 290, 288 and 290 us,
+// with margins of an eighth, a 16th and a 32nd of a part 306, 288 and 289 us.
 //
 // How large it gets: a call has some 2^30 (token, head) rows at most (of more, queries and results would not fit the memory), so 2^22
 // full units, each counted with up to 2^10 (2^30 + 2^9) + 2^30, and the last units of sequences add little: 4096 times the kv heads, with G
